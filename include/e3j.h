@@ -309,6 +309,50 @@ int e3j_conv_radial_bwd(const e3j_plan* plan, int64_t n_nodes, int64_t n_edges, 
                         const int32_t* colptr, const float* grad_out, float* grad_x, float* grad_sh,
                         float* grad_h, float* grad_W, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Hidden layers of the radial network (paper, "Key operations in scope": a radial-basis embedding followed by a multi-layer
+ * perceptron): what stands between the embedding of the distance and the activations h of e3j_conv_radial_*.  Rows are edges
+ * (or nodes).  All tensors of a call have the type `dtype`; sums are held in float32 and rounded once where they are
+ * stored.  Tensors are contiguous, row after row, and need only their natural alignment (4 or 2 bytes; rows that start on 16
+ * bytes are faster).  An input must not overlap an output.
+ *   n_real: DEVICE word with the number of real rows of a padded list (rowptr[n_nodes] of e3j_graph_prepare_padded), or NULL: all
+ *   rows are real.  Nothing of the rows behind it is read; their rows of y and grad_x are zeros and the parameters'
+ *   gradients leave them out.  Values below 0 count as 0, above `rows` as `rows`.
+ * Activations: y = z, z / (1 + exp(-z)), tanh(z), z (1 + erf(z / sqrt 2)) / 2.
+ * Results are bit-identical from run to run.  */
+#define E3J_F32 0
+#define E3J_BF16 1
+#define E3J_ACT_NONE 0
+#define E3J_ACT_SILU 1
+#define E3J_ACT_TANH 2
+#define E3J_ACT_GELU 3
+
+/* Linear layer: y = act(x W + b) + residual with x [rows, n_in], W [n_in, n_out], b [n_out] or NULL, residual [rows, n_out] or
+ * NULL, y [rows, n_out]; widths from 1 to 4096.  The products run on the tensor cores with float32 accuracy for float32 tensors (each
+ * as the sum of three bfloat16 terms); a row with an infinity or a NaN in x comes out as NaN.
+ * Backward: gz = grad_y act'(x W + b), formed again from x, W and b (the forward keeps nothing); grad_x = gz W^T, grad_W = x^T gz,
+ * grad_b = sum over rows of gz; the residual's gradient is grad_y itself.  Any of grad_x, grad_W, grad_b may be NULL (not wanted).
+ * Workspace: 256-byte aligned, e3j_linear_bwd_workspace_bytes(); calls that overlap on the GPU must not share it.
+ * e3j_linear_status reads (and clears) the status word of these kernels on the current device into the HOST word *status: 0 =
+ * fine, 1 = a bounded wait gave up and the outputs of some call are invalid.  Synchronises the device. */
+int e3j_linear_fwd(int dtype, int64_t rows, int n_in, int n_out, const void* x, const void* W, const void* b,
+                   const void* residual, int act, const int32_t* n_real, void* y, void* stream);
+size_t e3j_linear_bwd_workspace_bytes(int dtype, int64_t rows, int n_in, int n_out, int act);
+int e3j_linear_bwd(int dtype, int64_t rows, int n_in, int n_out, const void* x, const void* W, const void* b, const void* grad_y,
+                   int act, const int32_t* n_real, void* grad_x, void* grad_W, void* grad_b, void* workspace,
+                   size_t workspace_bytes, void* stream);
+int e3j_linear_status(int32_t* status);
+
+/* Layer norm over the n columns of a row (1 to 4096), with an activation behind it: z = (x - mean) / sqrt(variance + eps) * weight +
+ * bias, y = act(z); weight and bias [n], either may be NULL (1 and 0); eps >= 0.  Backward: the gradients of x, weight and bias from
+ * x, weight, bias and grad_y (mean and variance are formed again); any of grad_x, grad_weight, grad_bias may be NULL (not wanted).
+ * Workspace: 256-byte aligned, e3j_layer_norm_bwd_workspace_bytes(), needed where grad_weight or grad_bias is wanted. */
+int e3j_layer_norm_fwd(int dtype, int64_t rows, int n, const void* x, const void* weight, const void* bias, double eps, int act,
+                       const int32_t* n_real, void* y, void* stream);
+size_t e3j_layer_norm_bwd_workspace_bytes(int dtype, int64_t rows, int n);
+int e3j_layer_norm_bwd(int dtype, int64_t rows, int n, const void* x, const void* weight, const void* bias, const void* grad_y,
+                       double eps, int act, const int32_t* n_real, void* grad_x, void* grad_weight, void* grad_bias,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
 /* Standalone channelwise tensor product with per-row, per-path weights (paper:
  * tensor-product formula followed by the edge-scalar weighting; backward: the
  * tensor-product backward rule, one streaming pass).  Rows are their own receivers:

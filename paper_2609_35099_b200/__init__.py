@@ -30,13 +30,18 @@ __all__ = [
     "e3j_conv_radial_bwd_workspace_bytes",
     "e3j_conv_radial_fwd", "e3j_conv_radial_bwd", "e3j_conv_radial_vec_fwd", "e3j_conv_radial_vec_fwd_workspace_bytes", "e3j_conv_radial_vec_fwd_least_workspace_bytes", "e3j_conv_radial_vec_bwd", "e3j_conv_radial_vec_bwd_workspace_bytes",
     "e3j_tp_fwd", "e3j_tp_bwd", "e3j_bwd_schedule_bytes", "e3j_bwd_schedule_build", "e3j_conv_bwd_scheduled", "e3j_harmonics_fwd", "e3j_harmonics_bwd", "e3j_conv_vec_fwd", "e3j_conv_vec_bwd",
-    "e3j_conv_vec_fwd_workspace_bytes", "e3j_conv_vec_bwd_workspace_bytes", "e3j_conv_fwd_f64", "e3j_conv_bwd_f64", "e3j_shard_prepare", "e3j_rows_gather", "e3j_rows_add", "e3j_status_string", "e3j_selftest_bounded_wait", "e3j_launch_count", "E3J_PLAN_GENERIC_ONLY",
+    "e3j_conv_vec_fwd_workspace_bytes", "e3j_conv_vec_bwd_workspace_bytes", "e3j_conv_fwd_f64", "e3j_conv_bwd_f64", "e3j_shard_prepare", "e3j_rows_gather", "e3j_rows_add", "e3j_linear_fwd", "e3j_linear_bwd", "e3j_linear_bwd_workspace_bytes", "e3j_linear_status",
+    "e3j_layer_norm_fwd", "e3j_layer_norm_bwd", "e3j_layer_norm_bwd_workspace_bytes",
+    "e3j_status_string", "e3j_selftest_bounded_wait", "e3j_launch_count", "E3J_PLAN_GENERIC_ONLY",
     "E3J_PLAN_COLLAPSE_OUTPUTS", "E3J_PLAN_RADIAL_MATERIALISE",
+    "E3J_ACT_NONE", "E3J_ACT_SILU", "E3J_ACT_TANH", "E3J_ACT_GELU",
 ]
 
 E3J_PLAN_GENERIC_ONLY = 1
 E3J_PLAN_COLLAPSE_OUTPUTS = 2
 E3J_PLAN_RADIAL_MATERIALISE = 4
+E3J_F32, E3J_BF16 = 0, 1
+E3J_ACT_NONE, E3J_ACT_SILU, E3J_ACT_TANH, E3J_ACT_GELU = 0, 1, 2, 3
 # status codes of include/e3j.h
 E3J_OK, E3J_ERR_INVALID_ARG, E3J_ERR_BAD_IRREPS, E3J_ERR_MUL_NOT_UNIFORM = 0, -1, -2, -3
 E3J_ERR_UNSUPPORTED, E3J_ERR_WORKSPACE, E3J_ERR_CUDA, E3J_ERR_GRAPH = -4, -5, -6, -7
@@ -129,6 +134,20 @@ def _load():
     lib.e3j_conv_radial_vec_bwd.restype = i32
     lib.e3j_conv_radial_bwd.argtypes = [vp, i64, i64, i32] + [vp] * 15 + [sz, vp]
     lib.e3j_conv_radial_bwd.restype = i32
+    lib.e3j_linear_fwd.argtypes = [i32, i64, i32, i32] + [vp] * 4 + [i32] + [vp] * 3
+    lib.e3j_linear_fwd.restype = i32
+    lib.e3j_linear_bwd_workspace_bytes.argtypes = [i32, i64, i32, i32, i32]
+    lib.e3j_linear_bwd_workspace_bytes.restype = sz
+    lib.e3j_linear_bwd.argtypes = [i32, i64, i32, i32] + [vp] * 4 + [i32] + [vp] * 5 + [sz, vp]
+    lib.e3j_linear_bwd.restype = i32
+    lib.e3j_linear_status.argtypes = [ctypes.POINTER(ctypes.c_int32)]
+    lib.e3j_linear_status.restype = i32
+    lib.e3j_layer_norm_fwd.argtypes = [i32, i64, i32] + [vp] * 3 + [ctypes.c_double, i32] + [vp] * 3
+    lib.e3j_layer_norm_fwd.restype = i32
+    lib.e3j_layer_norm_bwd_workspace_bytes.argtypes = [i32, i64, i32]
+    lib.e3j_layer_norm_bwd_workspace_bytes.restype = sz
+    lib.e3j_layer_norm_bwd.argtypes = [i32, i64, i32] + [vp] * 4 + [ctypes.c_double, i32] + [vp] * 5 + [sz, vp]
+    lib.e3j_layer_norm_bwd.restype = i32
     lib.e3j_tp_fwd.argtypes = [vp, i64] + [vp] * 5
     lib.e3j_tp_bwd.argtypes = [vp, i64] + [vp] * 8
     lib.e3j_harmonics_fwd.argtypes = [i32, i64, vp, vp, vp]
@@ -197,6 +216,16 @@ def _run(entry: str, *args) -> None:
         status = getattr(_load(), entry)(*args)
     else:
         status = _native.call(_addresses.get(entry) or _address(entry), *args)
+    if status < 0:
+        raise E3JError(status, entry)
+
+
+def _run_real(entry: str, position: int, value: float, *args) -> None:
+    """_run for an entry point with a parameter of type double, the one at `position`."""
+    if _native is None:
+        status = getattr(_load(), entry)(*args[:position], value, *args[position:])
+    else:
+        status = _native.call_real(value, _addresses.get(entry) or _address(entry), *args)
     if status < 0:
         raise E3JError(status, entry)
 
@@ -702,6 +731,126 @@ def e3j_conv_radial_vec_bwd(plan: Plan, x, edge_vec, h, W, senders, receivers, g
         _dev_ptr(grad_h, f32, (e, hidden), "grad_h"), _dev_ptr(grad_W, f32, s_w, "grad_W"),
         workspace.data_ptr(), workspace.numel(), _stream(stream))
     return grad_x, grad_vec, grad_h, grad_W
+
+
+# ----------------------------------------------------------------- the radial network's hidden layers
+_layer_types = {}   # torch.float32 -> E3J_F32, ...
+
+
+def _layer_call(x, tensors, stream):
+    """The type code of a call on x [rows, n], and the context it runs in: None where x's device is the current one.  Every
+    other tensor has to be on that device too."""
+    torch = _torch()
+    if not _layer_types:
+        _layer_types.update({torch.float32: E3J_F32, torch.bfloat16: E3J_BF16})
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError("x must be a CUDA tensor")
+    code = _layer_types.get(x.dtype)
+    if code is None:
+        raise TypeError("x must be float32 or bfloat16")
+    if x.dim() != 2:
+        raise ValueError(f"x has shape {tuple(x.shape)}, expected [rows, columns]")
+    device = x.get_device()
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.get_device() != device:
+            raise ValueError("all tensors of a call must be on the same device")
+    if stream is not None and getattr(stream, "device_index", device) != device:
+        raise ValueError("the stream belongs to another device than the tensors")
+    return code, None if device == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _wanted(flag, shape, dtype, like):
+    """An output argument: True (allocate), False / None (not wanted) or a preallocated tensor."""
+    return _empty(shape, dtype, like) if flag is True else None if flag is False else flag
+
+
+def e3j_linear_fwd(x, W, b=None, residual=None, act: int = E3J_ACT_NONE, n_real=None, out=None, stream=None):
+    """act(x W + b) + residual: x [rows, n_in], W [n_in, n_out], b [n_out], residual [rows, n_out], all float32 or all
+    bfloat16.  n_real: int32 CUDA tensor of one element, the number of real rows of a padded list (rowptr[-1:]); the
+    rows of the result behind them are zeros."""
+    code, elsewhere = _layer_call(x, (W, b, residual, n_real, out), stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return e3j_linear_fwd(x, W, b, residual, act, n_real, out, stream)
+    dtype, (rows, n_in), n_out = x.dtype, x.shape, W.shape[-1]
+    if out is None:
+        out = _empty((rows, n_out), dtype, x)
+    _run("e3j_linear_fwd", code, rows, n_in, n_out, _dev_ptr(x, dtype, None, "x"), _dev_ptr(W, dtype, (n_in, n_out), "W"),
+         _dev_ptr(b, dtype, (n_out,), "b"), _dev_ptr(residual, dtype, (rows, n_out), "residual"), act,
+         _dev_ptr(n_real, _torch_module.int32, (1,), "n_real"), _dev_ptr(out, dtype, (rows, n_out), "out"), _stream(stream))
+    return out
+
+
+def e3j_linear_bwd_workspace_bytes(rows: int, n_in: int, n_out: int, act: int = E3J_ACT_NONE, dtype: int = E3J_F32) -> int:
+    return int(_load().e3j_linear_bwd_workspace_bytes(dtype, rows, n_in, n_out, act))
+
+
+def e3j_linear_bwd(x, W, b, grad_y, act: int = E3J_ACT_NONE, n_real=None, grad_x=True, grad_W=True, grad_b=True,
+                   workspace=None, stream=None):
+    """(grad_x, grad_W, grad_b) of e3j_linear_fwd from its inputs and grad_y (the residual's gradient is grad_y); each grad_*
+    argument is True (allocate), False/None (not wanted) or a preallocated tensor."""
+    code, elsewhere = _layer_call(x, (W, b, grad_y, n_real, grad_x, grad_W, grad_b, workspace), stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return e3j_linear_bwd(x, W, b, grad_y, act, n_real, grad_x, grad_W, grad_b, workspace, stream)
+    dtype, (rows, n_in), n_out = x.dtype, x.shape, W.shape[-1]
+    grad_x, grad_W = _wanted(grad_x, (rows, n_in), dtype, x), _wanted(grad_W, (n_in, n_out), dtype, x)
+    grad_b = _wanted(grad_b, (n_out,), dtype, x)
+    workspace = _workspace(int(_load().e3j_linear_bwd_workspace_bytes(code, rows, n_in, n_out, act)), x, workspace, stream)
+    _run("e3j_linear_bwd", code, rows, n_in, n_out, _dev_ptr(x, dtype, None, "x"), _dev_ptr(W, dtype, (n_in, n_out), "W"),
+         _dev_ptr(b, dtype, (n_out,), "b"), _dev_ptr(grad_y, dtype, (rows, n_out), "grad_y"), act,
+         _dev_ptr(n_real, _torch_module.int32, (1,), "n_real"), _dev_ptr(grad_x, dtype, (rows, n_in), "grad_x"),
+         _dev_ptr(grad_W, dtype, (n_in, n_out), "grad_W"), _dev_ptr(grad_b, dtype, (n_out,), "grad_b"),
+         workspace.data_ptr(), workspace.numel(), _stream(stream))
+    return grad_x, grad_W, grad_b
+
+
+def e3j_linear_status() -> int:
+    """Status of the linear layer's kernels on the current device since the last call (0 = fine); synchronises."""
+    st = ctypes.c_int32(0)
+    _check(_load().e3j_linear_status(ctypes.byref(st)), "e3j_linear_status")
+    return int(st.value)
+
+
+def e3j_layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, act: int = E3J_ACT_NONE, n_real=None, out=None,
+                       stream=None):
+    """act((x - mean) / sqrt(variance + eps) * weight + bias) over the columns of x [rows, n], all float32 or all bfloat16;
+    n_real as in e3j_linear_fwd."""
+    code, elsewhere = _layer_call(x, (weight, bias, n_real, out), stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return e3j_layer_norm_fwd(x, weight, bias, eps, act, n_real, out, stream)
+    dtype, (rows, n) = x.dtype, x.shape
+    if out is None:
+        out = _empty((rows, n), dtype, x)
+    _run_real("e3j_layer_norm_fwd", 6, float(eps), code, rows, n, _dev_ptr(x, dtype, None, "x"), _dev_ptr(weight, dtype, (n,), "weight"),
+              _dev_ptr(bias, dtype, (n,), "bias"), act, _dev_ptr(n_real, _torch_module.int32, (1,), "n_real"),
+              _dev_ptr(out, dtype, (rows, n), "out"), _stream(stream))
+    return out
+
+
+def e3j_layer_norm_bwd_workspace_bytes(rows: int, n: int, dtype: int = E3J_F32) -> int:
+    return int(_load().e3j_layer_norm_bwd_workspace_bytes(dtype, rows, n))
+
+
+def e3j_layer_norm_bwd(x, weight, bias, grad_y, eps: float = 1e-5, act: int = E3J_ACT_NONE, n_real=None, grad_x=True,
+                       grad_weight=True, grad_bias=True, workspace=None, stream=None):
+    """(grad_x, grad_weight, grad_bias) of e3j_layer_norm_fwd from its inputs and grad_y; each grad_* argument is True (allocate),
+    False/None (not wanted) or a preallocated tensor."""
+    code, elsewhere = _layer_call(x, (weight, bias, grad_y, n_real, grad_x, grad_weight, grad_bias, workspace), stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return e3j_layer_norm_bwd(x, weight, bias, grad_y, eps, act, n_real, grad_x, grad_weight, grad_bias, workspace, stream)
+    dtype, (rows, n) = x.dtype, x.shape
+    grad_x, grad_weight = _wanted(grad_x, (rows, n), dtype, x), _wanted(grad_weight, (n,), dtype, x)
+    grad_bias = _wanted(grad_bias, (n,), dtype, x)
+    workspace = _workspace(int(_load().e3j_layer_norm_bwd_workspace_bytes(code, rows, n)), x, workspace, stream)
+    _run_real("e3j_layer_norm_bwd", 7, float(eps), code, rows, n, _dev_ptr(x, dtype, None, "x"), _dev_ptr(weight, dtype, (n,), "weight"),
+              _dev_ptr(bias, dtype, (n,), "bias"), _dev_ptr(grad_y, dtype, (rows, n), "grad_y"), act,
+              _dev_ptr(n_real, _torch_module.int32, (1,), "n_real"), _dev_ptr(grad_x, dtype, (rows, n), "grad_x"),
+              _dev_ptr(grad_weight, dtype, (n,), "grad_weight"), _dev_ptr(grad_bias, dtype, (n,), "grad_bias"),
+              workspace.data_ptr(), workspace.numel(), _stream(stream))
+    return grad_x, grad_weight, grad_bias
 
 
 def e3j_tp_fwd(plan: Plan, x1, x2, w, out=None, stream=None):

@@ -87,8 +87,8 @@ PyObject* empty(PyObject*, PyObject* const* args, Py_ssize_t n) {
 // integer or a pointer and has a 64-bit slot of its own in the calling convention, so one signature serves all entry
 // points; slots behind the last are not read.  None is NULL, for the first `pointers` arguments alone.
 constexpr int kMostArgs = 24;
-template <class R>
-bool invoke(PyObject* const* args, Py_ssize_t n, Py_ssize_t pointers, R& result) {
+template <class R, class... Real>
+bool invoke(PyObject* const* args, Py_ssize_t n, Py_ssize_t pointers, R& result, Real... real) {
     if (n < 1 || n > kMostArgs + 1) {
         PyErr_SetString(PyExc_TypeError, "an address and up to 24 arguments");
         return false;
@@ -100,10 +100,10 @@ bool invoke(PyObject* const* args, Py_ssize_t n, Py_ssize_t pointers, R& result)
         if (v[i] == (uint64_t)-1 && PyErr_Occurred()) return false;
     }
     using U = uint64_t;
-    using Entry = R (*)(U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U);
+    using Entry = R (*)(Real..., U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U);
     const Entry f = reinterpret_cast<Entry>((uintptr_t)v[0]);
     Py_BEGIN_ALLOW_THREADS
-    result = f(v[1], v[2], v[3], v[4], v[5], v[6], v[7], v[8], v[9], v[10], v[11], v[12], v[13], v[14], v[15], v[16], v[17],
+    result = f(real..., v[1], v[2], v[3], v[4], v[5], v[6], v[7], v[8], v[9], v[10], v[11], v[12], v[13], v[14], v[15], v[16], v[17],
                v[18], v[19], v[20], v[21], v[22], v[23], v[24]);
     Py_END_ALLOW_THREADS
     return true;
@@ -115,6 +115,19 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyObject* call_size(PyObject*, PyObject* const* args, Py_ssize_t n) {
     size_t bytes;
     return invoke(args, n, 1, bytes) ? PyLong_FromSize_t(bytes) : nullptr;
+}
+
+// call_real(value, address, arguments...) -> status: for entry points with one parameter of type double, which travels in the first
+// floating-point register wherever it stands in the list, so the integers and pointers keep their slots.
+PyObject* call_real(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n < 2 || n > kMostArgs + 2) {
+        PyErr_SetString(PyExc_TypeError, "a number, an address and up to 24 arguments");
+        return nullptr;
+    }
+    const double value = PyFloat_AsDouble(args[0]);
+    if (value == -1.0 && PyErr_Occurred()) return nullptr;
+    int status;
+    return invoke(args + 1, n - 1, kMostArgs, status, value) ? PyLong_FromLong(status) : nullptr;
 }
 
 // set_slow(dev_ptr, empty): what the two functions above fall back on
@@ -133,6 +146,7 @@ PyObject* set_slow(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef methods[] = {
     {"dev_ptr", (PyCFunction)(void (*)(void))dev_ptr, METH_FASTCALL, nullptr},
     {"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, nullptr},
+    {"call_real", (PyCFunction)(void (*)(void))call_real, METH_FASTCALL, nullptr},
     {"call_size", (PyCFunction)(void (*)(void))call_size, METH_FASTCALL, nullptr},
     {"empty", (PyCFunction)(void (*)(void))empty, METH_FASTCALL, nullptr},
     {"set_slow", (PyCFunction)(void (*)(void))set_slow, METH_FASTCALL, nullptr},

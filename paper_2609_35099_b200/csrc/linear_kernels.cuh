@@ -1,0 +1,535 @@
+// Products of the linear layer on the fifth-generation tensor cores (sm_100a): forward, and the three products of its
+// backward, for float32 and bfloat16.
+//
+// Operands.  The tensor cores multiply bfloat16 pairs into float32 accumulators (tcgen05.mma kind::f16).  A float32 value is the
+// exact sum of three bfloat16 (24 significant bits are three times 8): v = hi + mid + lo, each the leading bits of what
+// is left, cut off and subtracted.  A product of two float32 is the sum of the six term products of weight 2^-16 and more; the
+// three left out are below 2^-22 of it.  That is as many tensor-core passes as the three-product TF32 form (whose products run at
+// half the rate), from 6 bytes of shared memory an element instead of 8, and with operands of 16 bits that the tensor cores take
+// along either dimension: x is the row operand of x W and the column operand of x^T gz from the same kind of image, with no
+// transposed copy of anything.  The float32 gradient gz of a bfloat16 layer is split into two terms (16 bits, the second rounded
+// to nearest), so it reaches both products of the backward without the loss of a rounding to bfloat16; bfloat16 tensors are one term.
+//
+// Image of a matrix block in shared memory: panels of 64 columns, 128 bytes a row, 16-byte pieces at (piece ^ row % 8): the 128-byte
+// swizzle.  With the panel's rows as the operand's rows it is K-major, with them as the contraction it is MN-major;
+// which, the instruction descriptor says.
+//
+// Accumulators.  The tensor cores add with truncation, so long chains drift (see radial_gemm.cuh).  Of float32 operands the
+// hi hi products go to one accumulator and the five smaller ones to another (B's hi and mid lie behind one another, so the first
+// two are one instruction of twice the width), and a chain ends after kGroupChunks chunks, 16 additions of hi hi: the epilogue adds groups in
+// float32 registers.
+//
+// Order of a tile's columns.  A quad of lanes reads tensor memory in pieces of 8 columns, two a lane (tcgen05.ld 16x256b).  Columns
+// of a 16-column group are dealt out so that the two pieces of a lane are four consecutive features: rows leave in 64-byte (float32) or
+// 32-byte (bfloat16) runs a quad, whole sectors, without a detour through shared memory.  (column_of)
+//
+// A block: 256 threads, all of which load, split and store operands and then read accumulators; thread 0 issues the tensor-core
+// instructions.  Two accumulator sets: while the tensor cores work on a tile, the block reads out the one before it and the loads
+// of the one after it are in flight; two blocks an SM fill each other's waits.  Waits are bounded (fast::mbar_wait).
+#pragma once
+#include "layer_common.cuh"
+#include "umma.cuh"
+
+namespace e3j {
+namespace layer {
+
+constexpr int kLinThreads = 256;
+constexpr int kTileRows = 128;      // accumulator lanes
+constexpr int kChunk = 64;          // contraction elements a chunk
+constexpr int kGroupChunks = 4;     // chunks a chain (float32 sums over rows)
+constexpr int kPanelBytes = 64 * 128;   // 64 rows of a panel
+
+enum Product { kForward, kSlope, kGradX, kGradW };
+// kForward  y = act(x W + b) + residual
+// kSlope    gz = grad_y act'(x W + b), float32, into the workspace
+// kGradX    grad_x = gz W^T
+// kGradW    shares of x^T gz and of the column sums of gz, one a range of rows
+
+struct LinArgs {
+    int64_t rows;
+    int n_in, n_out, act;
+    const int32_t* n_real;
+    const void *x, *W, *b, *residual, *grad_y;
+    const void* gz;        // kGradX, kGradW: grad_y itself where there is no activation
+    int ld_gz;             // elements between its rows
+    void* out;
+    float* shares;         // kGradW: [ranges][n_in * n_out + n_out]
+    int ranges, want_sums;
+    int n_tiles;           // tiles of 128 (kGradW: of its two dimensions, n_tiles x m_tiles) or NT columns
+    int m_tiles;
+    int stages, resident;  // operand stages; B's chunks stay in shared memory
+    unsigned vector;       // which arrays' rows start on 16 bytes: bit 0 A, 1 B, 2 out, 3 residual / grad_y
+    int32_t* status;
+};
+
+// ---------------------------------------------------------------- operands
+template <class T> struct Piece;   // 8 elements as they lie in memory
+template <> struct Piece<float> { float v[8]; };
+template <> struct Piece<bf16> { uint32_t v[4]; };
+
+__device__ __forceinline__ void load_piece(Piece<float>& p, const float* from, int left, bool vector) {
+    if (left >= 8 && vector) {
+        const float4 a = __ldg(reinterpret_cast<const float4*>(from)), b = __ldg(reinterpret_cast<const float4*>(from) + 1);
+        p.v[0] = a.x; p.v[1] = a.y; p.v[2] = a.z; p.v[3] = a.w; p.v[4] = b.x; p.v[5] = b.y; p.v[6] = b.z; p.v[7] = b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p.v[i] = i < left ? __ldg(from + i) : 0.f;
+    }
+}
+__device__ __forceinline__ void load_piece(Piece<bf16>& p, const bf16* from, int left, bool vector) {
+    if (left >= 8 && vector) {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(from));
+        p.v[0] = a.x; p.v[1] = a.y; p.v[2] = a.z; p.v[3] = a.w;
+    } else {
+        const uint16_t* const h = reinterpret_cast<const uint16_t*>(from);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            p.v[i] = (2 * i < left ? (uint32_t)__ldg(h + 2 * i) : 0u) | (2 * i + 1 < left ? (uint32_t)__ldg(h + 2 * i + 1) << 16 : 0u);
+    }
+}
+__device__ __forceinline__ float element(const Piece<float>& p, int i) { return p.v[i]; }
+__device__ __forceinline__ float element(const Piece<bf16>& p, int i) { return i & 1 ? high_float(p.v[i / 2]) : low_float(p.v[i / 2]); }
+
+// The terms of a piece, packed in pairs.
+__device__ __forceinline__ uint32_t cut_pair(float& a, float& b) {   // the leading 8 bits of both; what is left in a, b
+    const uint32_t p = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    a -= low_float(p);
+    b -= high_float(p);
+    return p;
+}
+template <int TERMS> __device__ __forceinline__ void split(const Piece<float>& p, uint32_t (&t)[TERMS][4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a = p.v[2 * i], b = p.v[2 * i + 1];
+#pragma unroll
+        for (int k = 0; k + 1 < TERMS; ++k) t[k][i] = cut_pair(a, b);
+        t[TERMS - 1][i] = pack_bf16(a, b);   // (exact as the third of three)
+    }
+}
+template <int TERMS> __device__ __forceinline__ void split(const Piece<bf16>& p, uint32_t (&t)[TERMS][4]) {
+    static_assert(TERMS == 1, "bfloat16 is one term");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[0][i] = p.v[i];
+}
+
+__device__ __forceinline__ uint32_t image_offset(int row, int piece) { return (uint32_t)(row * 128 + ((piece ^ (row & 7)) << 4)); }
+// where a feature of a 16-feature group lies among the tile's columns
+__device__ __forceinline__ int column_of(int f) { return 2 * ((f & 15) >> 2) + (f & 1) + ((f & 2) << 2) + (f & ~15); }
+
+// Matrix descriptor: 128-byte swizzle.  K-major: `stride` between groups of 8 rows (the other offset is not used).  MN-major:
+// `stride` between groups of 8 of the contraction, `leading` between panels.
+__device__ __forceinline__ uint64_t swizzled_desc(uint32_t address, uint32_t leading, uint32_t stride) {
+    const uint32_t lo = ((address >> 4) & 0x3FFFu) | (((leading >> 4) & 0x3FFFu) << 16);
+    const uint32_t hi = ((stride >> 4) & 0x3FFFu) | (1u << 14) | (2u << 29);
+    return ((uint64_t)hi << 32) | lo;
+}
+__host__ __device__ constexpr uint32_t idesc_bf16(int m, int n, bool a_mn, bool b_mn) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) |
+           ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// 16 lanes x 16 columns: v[0], v[1], v[4], v[5] are row lane / 4, the others row lane / 4 + 8; columns 2 (lane % 4) and the next one, of
+// the first and of the second 8.
+__device__ __forceinline__ void tmem_ld_quads(uint32_t taddr, float (&v)[8]) {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr) : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// Operand block of ROWS rows and COLS columns, taken in pieces of 8 columns (8 or 16 a row), or in pairs of pieces of 16 columns whose
+// order inside the group is column_of's (PERMUTED columns).
+template <class T, int TERMS, int ROWS, int COLS, bool PAIRS> struct Operand {
+    static constexpr int kWide = PAIRS ? 16 : 8;
+    static constexpr int kAcross = COLS / kWide;
+    static constexpr int kItems = ROWS * kAcross / kLinThreads;
+    static constexpr uint32_t kTermBytes = ROWS * COLS * 2;
+    static constexpr uint32_t kBytes = TERMS * kTermBytes;
+    static_assert(ROWS * kAcross % kLinThreads == 0, "the threads share the items");
+    Piece<T> p[kItems][PAIRS ? 2 : 1];
+
+    // rows [row0, row_end) and columns [col0, col_end) of `from` are there, the rest is zero
+    __device__ __forceinline__ void load(const T* from, int64_t ld, int64_t row0, int64_t row_end, int col0, int col_end, bool vector) {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const int item = i * kLinThreads + threadIdx.x;
+            const int64_t row = row0 + item / kAcross;
+            const int col = col0 + item % kAcross * kWide;
+            const T* const at = from + row * ld + col;
+            const int left = row < row_end ? col_end - col : 0;
+            load_piece(p[i][0], at, left, vector);
+            if constexpr (PAIRS) load_piece(p[i][1], at + 8, left - 8, vector);
+        }
+    }
+    // PERMUTE_ROWS: the block's rows become the tile's columns
+    template <bool PERMUTE_ROWS = false>
+    __device__ __forceinline__ void store(unsigned char* image) const {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const int item = i * kLinThreads + threadIdx.x;
+            int row = item / kAcross;
+            const int across = item % kAcross;
+            if constexpr (PERMUTE_ROWS) row = column_of(row);
+            uint32_t t[TERMS][4];
+            split<TERMS>(p[i][0], t);
+            if constexpr (!PAIRS) {
+                unsigned char* const at = image + (across >> 3) * (ROWS * 128) + image_offset(row, across & 7);
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k)
+                    *reinterpret_cast<uint4*>(at + k * kTermBytes) = make_uint4(t[k][0], t[k][1], t[k][2], t[k][3]);
+            } else {
+                uint32_t u[TERMS][4];
+                split<TERMS>(p[i][1], u);
+                unsigned char* const panel = image + (across >> 2) * (ROWS * 128);
+                const uint32_t even = image_offset(row, (across & 3) * 2), odd = image_offset(row, (across & 3) * 2 + 1);
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) {
+                    *reinterpret_cast<uint4*>(panel + k * kTermBytes + even) = make_uint4(t[k][0], t[k][2], u[k][0], u[k][2]);
+                    *reinterpret_cast<uint4*>(panel + k * kTermBytes + odd) = make_uint4(t[k][1], t[k][3], u[k][1], u[k][3]);
+                }
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------- the kernel
+// T: type of the layer's tensors; G: type of gz (kGradX, kGradW).
+template <Product P, class T, class G> struct Types {
+    using A = T; using B = T;
+    static constexpr int a_terms = sizeof(T) == 4 ? 3 : 1, b_terms = a_terms;
+};
+template <class T, class G> struct Types<kGradX, T, G> {
+    using A = G; using B = T;
+    static constexpr int b_terms = sizeof(T) == 4 ? 3 : 1, a_terms = sizeof(G) == 2 ? 1 : sizeof(T) == 4 ? 3 : 2;
+};
+template <class T, class G> struct Types<kGradW, T, G> {
+    using A = T; using B = G;
+    static constexpr int a_terms = sizeof(T) == 4 ? 3 : 1, b_terms = sizeof(G) == 2 ? 1 : sizeof(T) == 4 ? 3 : 2;
+};
+
+template <Product P, class T, class G, int NT> struct LinTile {
+    using Ty = Types<P, T, G>;
+    static constexpr bool kRowSum = P == kGradW;    // contraction over rows: both operands MN-major
+    using OpA = Operand<typename Ty::A, Ty::a_terms, kRowSum ? kChunk : kTileRows, kRowSum ? kTileRows : kChunk, false>;
+    using OpB = Operand<typename Ty::B, Ty::b_terms, P == kGradX ? NT : kChunk, P == kGradX ? kChunk : NT, P != kGradX>;
+    static constexpr bool kA_mn = kRowSum, kB_mn = P != kGradX;
+    static constexpr int kSets = Ty::a_terms == 3 ? 2 : 1;     // accumulators of a tile
+    static constexpr int kColumns = 2 * kSets * NT;            // tensor memory: two tiles
+    static constexpr int kBlocks = kColumns <= 256 ? 2 : 1;    // blocks an SM
+    static size_t smem_bytes(int stages, int b_slots) { return 1024 + (size_t)stages * OpA::kBytes + (size_t)b_slots * OpB::kBytes; }
+};
+
+template <Product P, class T, class G, int NT>
+__global__ void __launch_bounds__(kLinThreads, LinTile<P, T, G, NT>::kBlocks) linear_kernel(const __grid_constant__ LinArgs a) {
+    using L = LinTile<P, T, G, NT>;
+    using TA = typename L::Ty::A;
+    using TB = typename L::Ty::B;
+    using OpA = typename L::OpA;
+    using OpB = typename L::OpB;
+    constexpr int kTermsA = L::Ty::a_terms, kTermsB = L::Ty::b_terms;
+    extern __shared__ unsigned char raw_smem[];
+    __shared__ uint64_t stage_free[2], tile_done[2], drain;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_word, drain_word;
+    __shared__ float column_sums[P == kGradW ? 16 * NT : 1];
+    __shared__ float bias[P == kForward || P == kSlope ? NT : 1];
+    unsigned char* const smem = raw_smem + ((1024u - (umma::smem_addr(raw_smem) & 1023u)) & 1023u);
+    volatile int* const abort_flag = &abort_word;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) { fast::mbar_init(&stage_free[i], 1); fast::mbar_init(&tile_done[i], 1); }
+        fast::mbar_init(&drain, 1);
+        abort_word = drain_word = 0;
+        fast::mbar_fence_init();
+    }
+    if (warp == 0) umma::tmem_alloc(&tmem_slot, L::kColumns);
+    umma::fence_before_sync();
+    __syncthreads();
+    umma::fence_after_sync();
+    const uint32_t tmem = tmem_slot;
+    fast::grid_dependency_wait();
+    fast::grid_dependency_trigger();
+    const int64_t real = real_rows(a.rows, a.n_real);
+
+    // ---- what this block does: units (a tile, or for kGradW a group of chunks of one tile) of `chunks` chunks
+    const int nt = blockIdx.x % a.n_tiles;
+    const int n0 = nt * NT;
+    int units, chunks, m0 = 0;
+    int64_t unit0 = 0, unit_step = 1;          // row tiles of this block
+    int64_t chunk_begin = 0, chunk_end = 0;    // kGradW: chunks of rows of this block
+    if constexpr (P == kGradW) {
+        const int tile = blockIdx.x % (a.n_tiles * a.m_tiles), range = blockIdx.x / (a.n_tiles * a.m_tiles);
+        m0 = tile / a.n_tiles * kTileRows;
+        const int64_t all = (real + kChunk - 1) / kChunk;
+        chunk_begin = all * range / a.ranges;
+        chunk_end = all * (range + 1) / a.ranges;
+        units = (int)((chunk_end - chunk_begin + kGroupChunks - 1) / kGroupChunks);
+        chunks = kGroupChunks;
+    } else {
+        const int64_t tiles = (real + kTileRows - 1) / kTileRows;
+        unit0 = blockIdx.x / a.n_tiles;
+        unit_step = gridDim.x / a.n_tiles;
+        units = (int)(tiles > unit0 ? (tiles - unit0 + unit_step - 1) / unit_step : 0);
+        chunks = ((P == kGradX ? a.n_out : a.n_in) + kChunk - 1) / kChunk;
+    }
+    auto chunks_of = [&](int unit) {
+        if constexpr (P == kGradW) return (int)min((int64_t)kGroupChunks, chunk_end - chunk_begin - (int64_t)unit * kGroupChunks);
+        else return chunks;
+    };
+
+    OpA op_a;
+    OpB op_b;
+    auto load_a = [&](int unit, int chunk) {
+        const bool vec = a.vector & 1;
+        if constexpr (P == kGradW) {
+            const int64_t row0 = (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunk;
+            op_a.load((const TA*)a.x, a.n_in, row0, real, m0, a.n_in, vec);
+        } else {
+            const int64_t row0 = (unit0 + unit * unit_step) * kTileRows;
+            if constexpr (P == kGradX) op_a.load((const TA*)a.gz, a.ld_gz, row0, real, chunk * kChunk, a.n_out, vec);
+            else op_a.load((const TA*)a.x, a.n_in, row0, real, chunk * kChunk, a.n_in, vec);
+        }
+    };
+    auto load_b = [&](int unit, int chunk) {
+        const bool vec = a.vector & 2;
+        if constexpr (P == kGradW) {
+            const int64_t row0 = (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunk;
+            op_b.load((const TB*)a.gz, a.ld_gz, row0, real, n0, a.n_out, vec);
+        } else if constexpr (P == kGradX) {
+            op_b.load((const TB*)a.W, a.n_out, n0, a.n_in, chunk * kChunk, a.n_out, vec);
+        } else {
+            op_b.load((const TB*)a.W, a.n_out, chunk * kChunk, a.n_in, n0, a.n_out, vec);
+        }
+    };
+    unsigned char* const b_area = smem + (size_t)a.stages * OpA::kBytes;
+
+    if constexpr (P == kForward || P == kSlope)
+        if (threadIdx.x < NT)
+            bias[threadIdx.x] = a.b && n0 + (int)threadIdx.x < a.n_out ? to_float(((const T*)a.b)[n0 + threadIdx.x]) : 0.f;
+
+    // ---- accumulators -> registers -> memory
+    const int half = warp >> 2, quarter = warp & 3;
+    float sums[P == kGradW ? NT / 2 : 1];
+#pragma unroll
+    for (int i = 0; i < (P == kGradW ? NT / 2 : 1); ++i) sums[i] = 0.f;
+    auto read_out = [&](int unit, int set) {
+#pragma unroll
+        for (int c = 0; c < NT / 2; c += 16) {
+            const int col = half * (NT / 2) + c;              // of the tile
+            const int f = n0 + col + 4 * (lane & 3);          // first of this lane's four features
+            if (P != kGradW && n0 + col >= (P == kGradX ? a.n_in : a.n_out)) break;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {                     // 16 of the warp's 32 lanes of tensor memory
+                const uint32_t taddr = tmem + ((uint32_t)(quarter * 32 + h * 16) << 16) + (uint32_t)(set * L::kSets * NT + col);
+                float v[8];
+                __syncwarp();
+                tmem_ld_quads(taddr, v);
+                if constexpr (L::kSets == 2) {
+                    float u[8];
+                    tmem_ld_quads(taddr + NT, u);
+                    umma::tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] += u[i];
+                } else {
+                    umma::tmem_ld_wait();
+                }
+                if constexpr (P == kGradW) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sums[(c / 16 * 2 + h) * 8 + i] += v[i];
+                } else {
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const int64_t row = (unit0 + unit * unit_step) * kTileRows + quarter * 32 + h * 16 + s * 8 + lane / 4;
+                        float z[4] = {v[2 * s], v[2 * s + 1], v[4 + 2 * s], v[5 + 2 * s]};
+                        if constexpr (P == kForward || P == kSlope)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) z[i] += bias[col + 4 * (lane & 3) + i];
+                        if (row >= real) continue;
+                        const int width = P == kGradX ? a.n_in : a.n_out;
+                        const bool whole = f + 4 <= width;
+                        if constexpr (P == kForward) {
+                            activate(z, a.act);
+                            if (a.residual) {
+                                const T* const at = (const T*)a.residual + row * width + f;
+                                if (whole && (a.vector & 8)) {
+                                    float r[4];
+                                    Pack<T, 4>::load(r, at);
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) z[i] += r[i];
+                                } else {
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) if (f + i < width) z[i] += to_float(at[i]);
+                                }
+                            }
+                        }
+                        if constexpr (P == kSlope) {
+                            const T* const at = (const T*)a.grad_y + row * width + f;
+                            float g[4];
+                            if (whole && (a.vector & 8)) Pack<T, 4>::load(g, at);
+                            else
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) g[i] = f + i < width ? to_float(at[i]) : 0.f;
+                            times_slope(g, z, a.act);
+                            // (rows of gz are padded to whole vectors)
+                            if (f < a.ld_gz) Pack<float, 4>::store((float*)a.out + row * a.ld_gz + f, g);
+                        } else {
+                            T* const at = (T*)a.out + row * width + f;
+                            if (whole && (a.vector & 4)) Pack<T, 4>::store(at, z);
+                            else
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) if (f + i < width) at[i] = from_float<T>(z[i]);
+                        }
+                    }
+                }
+            }
+        }
+        umma::fence_before_sync();
+    };
+
+    // ---- the pipeline
+    float col_sum[P == kGradW ? 16 : 1];
+#pragma unroll
+    for (int i = 0; i < (P == kGradW ? 16 : 1); ++i) col_sum[i] = 0.f;
+    const uint32_t a_addr = umma::smem_addr(smem), b_addr = umma::smem_addr(b_area);
+    uint32_t step = 0;   // chunks so far
+    if (units > 0) {
+        if (a.resident)
+            for (int k = 0; k < chunks; ++k) {
+                load_b(0, k);
+                op_b.template store<P == kGradX>(b_area + (size_t)k * OpB::kBytes);
+            }
+        else load_b(0, 0);
+        load_a(0, 0);
+    }
+    for (int unit = 0; unit < units; ++unit) {
+        const int n_chunks = chunks_of(unit);
+        const int set = unit & 1;
+        for (int chunk = 0; chunk < n_chunks; ++chunk, ++step) {
+            const int stage = a.stages == 2 ? step & 1 : 0;
+            const int b_slot = a.resident ? chunk : stage;
+            if (step >= (uint32_t)a.stages)   // the products that read this stage last are over
+                fast::mbar_wait(&stage_free[stage], ((step / a.stages) - 1) & 1, abort_flag, a.status);
+            op_a.store(smem + (size_t)stage * OpA::kBytes);
+            if (!a.resident) {
+                op_b.template store<P == kGradX>(b_area + (size_t)stage * OpB::kBytes);
+                if constexpr (P == kGradW) {
+                    if (a.want_sums && m0 == 0) {
+#pragma unroll
+                        for (int i = 0; i < OpB::kItems; ++i)
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) col_sum[j] += element(op_b.p[i][j >> 3], j & 7);
+                    }
+                }
+            }
+            umma::fence_smem_to_async();
+            umma::fence_before_sync();
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                umma::fence_after_sync();
+                const uint32_t d = tmem + (uint32_t)(set * L::kSets * NT);
+                const uint32_t pa = a_addr + stage * OpA::kBytes, pb = b_addr + b_slot * OpB::kBytes;
+                constexpr uint32_t a_step = L::kA_mn ? 2048 : 32, b_step = L::kB_mn ? 2048 : 32;
+                constexpr uint32_t one = idesc_bf16(kTileRows, NT, L::kA_mn, L::kB_mn);
+                constexpr uint32_t two = idesc_bf16(kTileRows, 2 * NT, L::kA_mn, L::kB_mn);
+                // k-steps that hold anything
+                int steps = kChunk / 16;
+                if constexpr (P != kGradW) steps = min(steps, ((P == kGradX ? a.n_out : a.n_in) - chunk * kChunk + 15) / 16);
+                for (int k = 0; k < steps; ++k) {
+                    const uint32_t add = chunk > 0 || k > 0;   // (else the accumulators are overwritten)
+                    auto da = [&](int term) { return swizzled_desc(pa + term * OpA::kTermBytes + k * a_step, kPanelBytes, 1024); };
+                    auto db = [&](int term) { return swizzled_desc(pb + term * OpB::kTermBytes + k * b_step, kPanelBytes, 1024); };
+                    if constexpr (kTermsA == 3) {
+                        mma_bf16(d, da(0), db(0), two, add);         // hi [hi | mid]
+                        mma_bf16(d + NT, da(1), db(0), one, 1);
+                        mma_bf16(d + NT, da(1), db(1), one, 1);
+                        mma_bf16(d + NT, da(0), db(2), one, 1);
+                        mma_bf16(d + NT, da(2), db(0), one, 1);
+                    } else {
+                        mma_bf16(d, da(0), db(0), one, add);
+                        if constexpr (kTermsA == 2) mma_bf16(d, da(1), db(0), one, 1);
+                        if constexpr (kTermsB == 2) mma_bf16(d, da(0), db(1), one, 1);
+                    }
+                }
+                umma::commit(&stage_free[stage]);
+                if (chunk + 1 == n_chunks) umma::commit(&tile_done[set]);
+            }
+            const bool more = chunk + 1 < n_chunks;
+            if (more || unit + 1 < units) {
+                load_a(more ? unit : unit + 1, more ? chunk + 1 : 0);
+                if (!a.resident) load_b(more ? unit : unit + 1, more ? chunk + 1 : 0);
+            }
+            if (chunk == 0 && unit > 0) {   // the tile before this one
+                fast::mbar_wait(&tile_done[set ^ 1], ((unit - 1) >> 1) & 1, abort_flag, a.status);
+                umma::fence_after_sync();
+                read_out(unit - 1, set ^ 1);
+            }
+        }
+    }
+    if (units > 0) {
+        fast::mbar_wait(&tile_done[(units - 1) & 1], ((units - 1) >> 1) & 1, abort_flag, a.status);
+        umma::fence_after_sync();
+        read_out(units - 1, (units - 1) & 1);
+    }
+
+    if constexpr (P == kGradW) {
+        const int range = blockIdx.x / (a.n_tiles * a.m_tiles);
+        float* const share = a.shares + (size_t)range * ((size_t)a.n_in * a.n_out + a.n_out);
+#pragma unroll
+        for (int c = 0; c < NT / 2; c += 16)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int row = m0 + quarter * 32 + h * 16 + ((i >> 1) & 1) * 8 + lane / 4;
+                    const int f = n0 + half * (NT / 2) + c + 4 * (lane & 3) + (i & 1) + ((i >> 2) << 1);
+                    if (row < a.n_in && f < a.n_out) share[(size_t)row * a.n_out + f] = sums[(c / 16 * 2 + h) * 8 + i];
+                }
+        if (a.want_sums && m0 == 0) {
+            // a thread's 16 columns are the same in every chunk: [16 or more row groups][NT]
+            constexpr int kAcross = OpB::kAcross, kGroups = kLinThreads / kAcross;
+            static_assert(kGroups == 32 || kGroups == 64, "");
+            const int across = threadIdx.x % kAcross, group = threadIdx.x / kAcross;
+            // groups of threads in turn, 16 at a time
+            for (int t = 0; t < kGroups / 16; ++t) {
+                if (group / 16 == t)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        float* const at = &column_sums[(group % 16) * NT + across * 16 + j];
+                        *at = t == 0 ? col_sum[j] : *at + col_sum[j];
+                    }
+                __syncthreads();
+            }
+            if (threadIdx.x < NT && n0 + (int)threadIdx.x < a.n_out) {
+                float s = 0.f;
+                for (int r = 0; r < 16; ++r) s += column_sums[r * NT + threadIdx.x];
+                share[(size_t)a.n_in * a.n_out + n0 + threadIdx.x] = s;
+            }
+        }
+    } else if (P != kSlope && real < a.rows) {
+        // zero rows behind the last real one
+        const int width = P == kGradX ? a.n_in : a.n_out;
+        T* const out = (T*)a.out;
+        for (int64_t i = real * width + blockIdx.x * (int64_t)kLinThreads + threadIdx.x; i < a.rows * width; i += (int64_t)gridDim.x * kLinThreads)
+            out[i] = from_float<T>(0.f);
+    }
+    if (threadIdx.x == 0 && *abort_flag) {   // a wait ran out: the tensor cores finish before tensor memory goes back
+        umma::commit(&drain);
+        fast::mbar_wait(&drain, 0, &drain_word, a.status);
+    }
+    umma::fence_before_sync();
+    __syncthreads();
+    umma::fence_after_sync();
+    if (warp == 0) umma::tmem_dealloc(tmem, L::kColumns);
+}
+
+}  // namespace layer
+}  // namespace e3j
