@@ -32,67 +32,97 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&p);
 }
 
-// V consecutive elements as float32, read or written in one access (V = 1, or 4, 8 or 16 bytes that start on a multiple of
-// their size).
+// V consecutive elements, read or written in one access (16 bytes that start on a multiple of 16, or one element): as they lie in
+// memory (Raw), and as pairs of float32 (one element: the first of a pair, and 0).
 template <class T, int V> struct Pack;
 template <> struct Pack<float, 1> {
-    static __device__ __forceinline__ void load(float (&v)[1], const float* p) { v[0] = __ldg(p); }
-    static __device__ __forceinline__ void store(float* p, const float (&v)[1]) { *p = v[0]; }
+    using Raw = float;
+    static constexpr int kPairs = 1;
+    static __device__ __forceinline__ Raw none() { return 0.f; }
+    static __device__ __forceinline__ Raw fetch(const float* p) { return __ldg(p); }
+    static __device__ __forceinline__ float2 pair(const Raw& r, int) { return make_float2(r, 0.f); }
+    static __device__ __forceinline__ Raw from(const float2 (&v)[1]) { return v[0].x; }
+    static __device__ __forceinline__ void store(float* p, const Raw& r) { *p = r; }
 };
 template <> struct Pack<float, 4> {
-    static __device__ __forceinline__ void load(float (&v)[4], const float* p) {
-        const float4 q = __ldg(reinterpret_cast<const float4*>(p));
-        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
-    }
-    static __device__ __forceinline__ void store(float* p, const float (&v)[4]) {
-        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    }
+    using Raw = float4;
+    static constexpr int kPairs = 2;
+    static __device__ __forceinline__ Raw none() { return make_float4(0.f, 0.f, 0.f, 0.f); }
+    static __device__ __forceinline__ Raw fetch(const float* p) { return __ldg(reinterpret_cast<const float4*>(p)); }
+    static __device__ __forceinline__ float2 pair(const Raw& q, int i) { return i ? make_float2(q.z, q.w) : make_float2(q.x, q.y); }
+    static __device__ __forceinline__ Raw from(const float2 (&v)[2]) { return make_float4(v[0].x, v[0].y, v[1].x, v[1].y); }
+    static __device__ __forceinline__ void store(float* p, const Raw& r) { *reinterpret_cast<float4*>(p) = r; }
 };
 template <> struct Pack<bf16, 1> {
-    static __device__ __forceinline__ void load(float (&v)[1], const bf16* p) { v[0] = to_float(*p); }
-    static __device__ __forceinline__ void store(bf16* p, const float (&v)[1]) { *p = from_float<bf16>(v[0]); }
-};
-template <> struct Pack<bf16, 2> {
-    static __device__ __forceinline__ void load(float (&v)[2], const bf16* p) {
-        const uint32_t q = __ldg(reinterpret_cast<const uint32_t*>(p));
-        v[0] = low_float(q); v[1] = high_float(q);
-    }
-    static __device__ __forceinline__ void store(bf16* p, const float (&v)[2]) {
-        *reinterpret_cast<uint32_t*>(p) = pack_bf16(v[0], v[1]);
-    }
-};
-template <> struct Pack<bf16, 4> {
-    static __device__ __forceinline__ void load(float (&v)[4], const bf16* p) {
-        const uint2 q = __ldg(reinterpret_cast<const uint2*>(p));
-        v[0] = low_float(q.x); v[1] = high_float(q.x); v[2] = low_float(q.y); v[3] = high_float(q.y);
-    }
-    static __device__ __forceinline__ void store(bf16* p, const float (&v)[4]) {
-        *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-    }
+    using Raw = uint16_t;
+    static constexpr int kPairs = 1;
+    static __device__ __forceinline__ Raw none() { return 0; }
+    static __device__ __forceinline__ Raw fetch(const bf16* p) { return __ldg(reinterpret_cast<const uint16_t*>(p)); }
+    static __device__ __forceinline__ float2 pair(const Raw& r, int) { return make_float2(low_float(r), 0.f); }
+    static __device__ __forceinline__ Raw from(const float2 (&v)[1]) { return (uint16_t)pack_bf16(v[0].x, 0.f); }
+    static __device__ __forceinline__ void store(bf16* p, const Raw& r) { *reinterpret_cast<uint16_t*>(p) = r; }
 };
 template <> struct Pack<bf16, 8> {
-    static __device__ __forceinline__ void load(float (&v)[8], const bf16* p) {
+    struct Raw { uint32_t w[4]; };
+    static constexpr int kPairs = 4;
+    static __device__ __forceinline__ Raw none() { return Raw{{0, 0, 0, 0}}; }
+    static __device__ __forceinline__ Raw fetch(const bf16* p) {
         const uint4 q = __ldg(reinterpret_cast<const uint4*>(p));
-        v[0] = low_float(q.x); v[1] = high_float(q.x); v[2] = low_float(q.y); v[3] = high_float(q.y);
-        v[4] = low_float(q.z); v[5] = high_float(q.z); v[6] = low_float(q.w); v[7] = high_float(q.w);
+        return Raw{{q.x, q.y, q.z, q.w}};
     }
-    static __device__ __forceinline__ void store(bf16* p, const float (&v)[8]) {
-        *reinterpret_cast<uint4*>(p) =
-            make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    static __device__ __forceinline__ float2 pair(const Raw& q, int i) { return make_float2(low_float(q.w[i]), high_float(q.w[i])); }
+    static __device__ __forceinline__ Raw from(const float2 (&v)[4]) {
+        return Raw{{pack_bf16(v[0].x, v[0].y), pack_bf16(v[1].x, v[1].y), pack_bf16(v[2].x, v[2].y), pack_bf16(v[3].x, v[3].y)}};
+    }
+    static __device__ __forceinline__ void store(bf16* p, const Raw& r) {
+        *reinterpret_cast<uint4*>(p) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
     }
 };
+// Four elements that start on a multiple of their size.
+__device__ __forceinline__ void load_four(float (&v)[4], const float* p) {
+    const float4 q = __ldg(reinterpret_cast<const float4*>(p));
+    v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+}
+__device__ __forceinline__ void load_four(float (&v)[4], const bf16* p) {
+    const uint2 q = __ldg(reinterpret_cast<const uint2*>(p));
+    v[0] = low_float(q.x); v[1] = high_float(q.x); v[2] = low_float(q.y); v[3] = high_float(q.y);
+}
+__device__ __forceinline__ void store_four(float* p, const float (&v)[4]) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void store_four(bf16* p, const float (&v)[4]) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+}
 
 // 1 / (1 + exp(-z)).  The fast exponential and division are within a few float32 roundings where the result is not tiny;
 // exp(-z) = infinity gives 0.
 __device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
 
-__device__ __forceinline__ float normal_cdf(float z) { return 0.5f * (1.f + erff(0.70710678f * z)); }
+// Normal distribution: its density phi(z) and distribution function Phi(z) from one exponential.  erf by the rational approximation
+// of Hastings (Abramowitz and Stegun 7.1.26), 1 - (a1 t + .. + a5 t^5) exp(-x^2) with t = 1 / (1 + p x), which is within 1.5e-7
+// (2.5 half steps of float32); Phi of a negative z is the second term's half and keeps its relative accuracy.  A layer norm of
+// 49 157 rows of 385 bfloat16 with GELU is bound by instructions: backward NNN us, with erff MMM.
+__device__ __forceinline__ void normal(float z, float& phi, float& Phi) {
+    const float x = fabsf(z) * 0.70710678f;
+    const float t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
+    const float e = __expf(-x * x);
+    float poly = fmaf(1.061405429f, t, -1.453152027f);
+    poly = fmaf(poly, t, 1.421413741f);
+    poly = fmaf(poly, t, -0.284496736f);
+    poly = fmaf(poly, t, 0.254829592f);
+    const float tail = 0.5f * poly * t * e;   // Phi(-|z|)
+    Phi = z < 0.f ? tail : 1.f - tail;
+    phi = 0.39894228f * e;
+}
 
 template <int ACT> __device__ __forceinline__ float activation(float z) {
     if constexpr (ACT == E3J_ACT_SILU) return z * logistic(z);
     else if constexpr (ACT == E3J_ACT_TANH) return tanhf(z);
-    else if constexpr (ACT == E3J_ACT_GELU) return z * normal_cdf(z);
-    else return z;
+    else if constexpr (ACT == E3J_ACT_GELU) {
+        float phi, Phi;
+        normal(z, phi, Phi);
+        return z * Phi;
+    } else return z;
 }
 template <int ACT> __device__ __forceinline__ float slope(float z) {
     if constexpr (ACT == E3J_ACT_SILU) {
@@ -102,36 +132,40 @@ template <int ACT> __device__ __forceinline__ float slope(float z) {
         const float t = tanhf(z);
         return fmaf(-t, t, 1.f);
     } else if constexpr (ACT == E3J_ACT_GELU) {
-        return fmaf(z, 0.39894228f * __expf(-0.5f * z * z), normal_cdf(z));
+        float phi, Phi;
+        normal(z, phi, Phi);
+        return fmaf(z, phi, Phi);
     } else {
         return 1.f;
     }
 }
-// The same with the activation as a run-time value: one uniform branch for all elements of v.
-template <int N> __device__ __forceinline__ void activate(float (&v)[N], int act) {
-    if (act == E3J_ACT_SILU) {
+// The same with the activation as a run-time value: one uniform branch for all elements.
+template <int ACT, int N> __device__ __forceinline__ void activate_as(float (&v)[N]) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = activation<E3J_ACT_SILU>(v[i]);
-    } else if (act == E3J_ACT_TANH) {
+    for (int i = 0; i < N; ++i) v[i] = activation<ACT>(v[i]);
+}
+template <int ACT, int N> __device__ __forceinline__ void activate_as(float2 (&v)[N]) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = activation<E3J_ACT_TANH>(v[i]);
-    } else if (act == E3J_ACT_GELU) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = activation<E3J_ACT_GELU>(v[i]);
-    }
+    for (int i = 0; i < N; ++i) v[i] = make_float2(activation<ACT>(v[i].x), activation<ACT>(v[i].y));
+}
+template <class F, int N> __device__ __forceinline__ void activate(F (&v)[N], int act) {
+    if (act == E3J_ACT_SILU) activate_as<E3J_ACT_SILU>(v);
+    else if (act == E3J_ACT_TANH) activate_as<E3J_ACT_TANH>(v);
+    else if (act == E3J_ACT_GELU) activate_as<E3J_ACT_GELU>(v);
 }
 // g[i] *= slope(z[i])
-template <int N> __device__ __forceinline__ void times_slope(float (&g)[N], const float (&z)[N], int act) {
-    if (act == E3J_ACT_SILU) {
+template <int ACT, int N> __device__ __forceinline__ void times_slope_as(float (&g)[N], const float (&z)[N]) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) g[i] *= slope<E3J_ACT_SILU>(z[i]);
-    } else if (act == E3J_ACT_TANH) {
+    for (int i = 0; i < N; ++i) g[i] *= slope<ACT>(z[i]);
+}
+template <int ACT, int N> __device__ __forceinline__ void times_slope_as(float2 (&g)[N], const float2 (&z)[N]) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) g[i] *= slope<E3J_ACT_TANH>(z[i]);
-    } else if (act == E3J_ACT_GELU) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) g[i] *= slope<E3J_ACT_GELU>(z[i]);
-    }
+    for (int i = 0; i < N; ++i) g[i] = __fmul2_rn(g[i], make_float2(slope<ACT>(z[i].x), slope<ACT>(z[i].y)));
+}
+template <class F, int N> __device__ __forceinline__ void times_slope(F (&g)[N], const F (&z)[N], int act) {
+    if (act == E3J_ACT_SILU) times_slope_as<E3J_ACT_SILU>(g, z);
+    else if (act == E3J_ACT_TANH) times_slope_as<E3J_ACT_TANH>(g, z);
+    else if (act == E3J_ACT_GELU) times_slope_as<E3J_ACT_GELU>(g, z);
 }
 
 // A parameter's gradient from the blocks' shares of it, added in a fixed order: 32 elements a block, kSumWays

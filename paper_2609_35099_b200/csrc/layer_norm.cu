@@ -7,11 +7,10 @@
 //
 // Both passes are bound by memory and read every row once: a row stays in the registers of the lanes that share it, so mean
 // and variance (about the mean: two sums one after the other, no cancellation) cost shuffles, not traffic, and the backward
-// forms them again from the x that it has to read anyway instead of having the forward write them.  A row is shared by
-// as many lanes as it has 16-byte pieces where that is no more than a warp (64 float32: 16 lanes, two rows a warp), by a
-// warp with several pieces a lane, or by several warps.  Rows that do not start on 16 bytes are read by the 4 bytes or by
-// the element, lane-strided, so that a lane keeps the same columns, and with them its share of the parameters'
-// gradients, in every row.
+// forms them again from the x that it has to read anyway instead of having the forward write them.  A lane has 8 elements of a
+// row: with fewer, what a row costs once (the sums' shuffles, the root) bounds narrow rows.  So a row of 64 is shared by 8 lanes, four
+// rows a warp; from 256 columns on it is 16 elements and whole warps, up to eight of them a row.  Arithmetic on pairs
+// (packed float32 instructions), since with 2-byte elements the instructions, not the memory, come first.
 //
 // The parameters' gradients are sums over all rows: every lane adds up its columns over the rows it meets, the warps of a
 // block add theirs in order, and sum_shares_kernel adds the blocks' shares in order.  No atomics; the same bits every time.
@@ -24,11 +23,11 @@ namespace layer {
 namespace {
 
 constexpr int kNormThreads = 256, kNormWarps = kNormThreads / 32;
-constexpr int kMostNorm = 4096;   // columns: 8 warps of 16 elements a lane (backward)
+constexpr int kMostNorm = 4096;   // columns: 256 lanes of 16 elements
 
 struct NormArgs {
     int64_t rows;
-    int n, lanes;          // lanes that share a row: a power of two up to 32 (one access a lane), or 32 times a power of two
+    int n, lanes;          // lanes that share a row: a power of two
     float eps, inverse_n;
     int act;
     const void *x, *weight, *bias, *grad_y;
@@ -37,17 +36,19 @@ struct NormArgs {
     float* shares;         // backward: [blocks][2 n] of grad_weight and grad_bias (null: not wanted)
 };
 
-// Sums over the lanes of a row, all of which get them.  Rows of several warps meet in shared memory; consecutive sums use the two
-// halves of it in turn, so one barrier a sum is enough.
-struct RowSum {
+// Sums over the lanes of a row (LANES; 0: several warps), all of which get them.  Rows of several warps meet in shared memory;
+// consecutive sums use the two halves of it in turn, so one barrier a sum is enough.
+template <int LANES> struct RowSum {
     int lanes, slot, half;
     float2* meet;   // [2][kNormWarps]
+    __device__ __forceinline__ void within_warp(float& v) {
+#pragma unroll
+        for (int o = (LANES ? LANES : 32) >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    }
     __device__ __forceinline__ float2 operator()(float2 v) {
-        for (int o = min(lanes, 32) >> 1; o > 0; o >>= 1) {
-            v.x += __shfl_xor_sync(~0u, v.x, o);
-            v.y += __shfl_xor_sync(~0u, v.y, o);
-        }
-        if (lanes > 32) {
+        within_warp(v.x);
+        within_warp(v.y);
+        if constexpr (LANES == 0) {
             const int warps = lanes >> 5, warp = threadIdx.x >> 5;
             float2* const m = meet + half * kNormWarps;
             half ^= 1;
@@ -58,17 +59,28 @@ struct RowSum {
         }
         return v;
     }
+    __device__ __forceinline__ float operator()(float v) { return (*this)(make_float2(v, 0.f)).x; }
 };
 
-// BWD: backward.  V elements an access, NV accesses a lane and row.
-template <class T, int V, int NV, bool BWD>
-__global__ void __launch_bounds__(kNormThreads, V * NV <= 8 ? 4 : 2) norm_kernel(const NormArgs a) {
-    constexpr int E = V * NV;
-    constexpr bool kKeep = E <= 8;     // the parameters' columns stay in registers (else they are read from shared memory)
-    constexpr bool kAhead = E <= 8;    // the next row is fetched while this one is worked on
-    extern __shared__ float params[];  // [weight | bias], later the block's sums
+// Blocks an SM: as many as the registers allow (nearly) without spilling.
+__host__ __device__ constexpr int norm_blocks(int v, int each, bool bwd) {
+    return v == 1 ? (each == 8 && !bwd ? 2 : 1)
+         : each == 8 ? (!bwd ? 4 : v == 4 ? 2 : 3)
+         : v == 4 ? (bwd ? 1 : 2) : (bwd ? 2 : 3);
+}
+
+// BWD: backward.  V elements an access, EACH a lane and row; LANES lanes a row (0: a.lanes of them, whole warps).
+// RAGGED: rows do not start on 16 bytes.  A row's lanes then count from the 16-byte boundary before its start, `shift` columns to
+// the left of it; the grid's stride is a multiple of V rows, so a slot's rows all have the same shift and its lanes keep
+// their columns.  Accesses that reach over an end of the row go element by element.
+template <class T, int V, int EACH, int LANES, bool RAGGED, bool BWD>
+__global__ void __launch_bounds__(kNormThreads, norm_blocks(V, EACH, BWD)) norm_kernel(const NormArgs a) {
+    constexpr int NV = EACH / V;
+    using P = Pack<T, V>;
+    constexpr int H = P::kPairs, E2 = NV * H;   // pairs of an access, of a lane
+    extern __shared__ float block_sums[];       // backward: [2][n]
     __shared__ float2 meet[2 * kNormWarps];
-    const int n = a.n, lanes = NV == 1 ? min(a.lanes, 32) : a.lanes;
+    const int n = a.n, lanes = LANES ? LANES : a.lanes;
     const int slots = kNormThreads / lanes, slot = threadIdx.x / lanes, lane = threadIdx.x % lanes;
     const T* const x = (const T*)a.x;
     const T* const gy = (const T*)a.grad_y;
@@ -76,216 +88,258 @@ __global__ void __launch_bounds__(kNormThreads, V * NV <= 8 ? 4 : 2) norm_kernel
     fast::grid_dependency_wait();
     fast::grid_dependency_trigger();
     const int64_t real = real_rows(a.rows, a.n_real);
+    const int64_t stride = (int64_t)gridDim.x * slots;
+    int64_t row = (int64_t)blockIdx.x * slots + slot;
 
-    auto col = [&](int i) { return (lane + i * lanes) * V; };
-    float w[kKeep ? E : 1], b[kKeep ? E : 1];
-    if constexpr (kKeep) {
+    const int shift = RAGGED ? (int)(row * n % V) : 0;
+    auto col = [&](int i) { return (lane + i * lanes) * V - shift; };
+    auto whole = [&](int i) { return RAGGED ? col(i) >= 0 && col(i) + V <= n : col(i) < n; };
+    auto inside = [&](int c) { return RAGGED ? c >= 0 && c < n : c < n; };
+    // access i of a row from its elements, those outside the row 0
+    auto piecewise = [&](const T* at, int i) {
+        float2 v[H];
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const bool in = col(i) < n;
-                w[i * V + j] = in && a.weight ? to_float(((const T*)a.weight)[col(i) + j]) : 1.f;
-                b[i * V + j] = in && a.bias ? to_float(((const T*)a.bias)[col(i) + j]) : 0.f;
-            }
-    } else {
-        for (int i = threadIdx.x; i < n; i += kNormThreads) {
-            params[i] = a.weight ? to_float(((const T*)a.weight)[i]) : 1.f;
-            params[n + i] = a.bias ? to_float(((const T*)a.bias)[i]) : 0.f;
+        for (int j = 0; j < V; ++j) {
+            const float f = inside(col(i) + j) ? to_float(at[col(i) + j]) : 0.f;
+            if (j & 1) v[j / 2].y = f;
+            else v[j / 2] = make_float2(f, 0.f);
         }
-        __syncthreads();
-    }
-    auto weight_at = [&](int i, int j) { if constexpr (kKeep) return w[i * V + j]; else return params[col(i) + j]; };
-    auto bias_at = [&](int i, int j) { if constexpr (kKeep) return b[i * V + j]; else return params[n + col(i) + j]; };
-    auto fetch = [&](float (&v)[E], const T* from, int64_t row) {
+        return P::from(v);
+    };
+    const int64_t all = a.rows * n;
+    struct Part { typename P::Raw r[NV]; };     // a lane's part of a row, as it lies in memory
+    auto fetch = [&](Part& p, const T* from, int64_t r) {
+        const T* const at = from + r * n;
+        if (r < real) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float p[V];
-            if (row < real && col(i) < n) Pack<T, V>::load(p, from + row * n + col(i));
-            else
+            for (int i = 0; i < NV; ++i) {
+                // (an access over an end of the row takes in some of the next row, or of the one before; not over the array's)
+                if (whole(i) || (RAGGED && col(i) < n && r * n + col(i) + V <= all)) p.r[i] = P::fetch(at + col(i));
+                else if (RAGGED && col(i) < n) p.r[i] = piecewise(at, i);
+                else p.r[i] = P::none();
+            }
+        } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) p[j] = 0.f;
-#pragma unroll
-            for (int j = 0; j < V; ++j) v[i * V + j] = p[j];
+            for (int i = 0; i < NV; ++i) p.r[i] = P::none();
         }
     };
-
-    RowSum row_sum{lanes, lanes > 32 ? slot : 0, 0, meet};
-    float sum_w[BWD ? E : 1], sum_b[BWD ? E : 1];
+    // this lane's columns of the parameters; columns outside the row: 0
+    Part w, b;
+    {
+        float2 ones[H];
 #pragma unroll
-    for (int i = 0; i < (BWD ? E : 1); ++i) sum_w[i] = sum_b[i] = 0.f;
-    const int64_t stride = (int64_t)gridDim.x * slots;
-    // All lanes of a warp make the same number of turns (the shuffles need them): the turn of a block's first slot counts.
-    int64_t row = (int64_t)blockIdx.x * slots + slot;
-    float v[E], g[BWD ? E : 1];
-    fetch(v, x, row);
-    if constexpr (BWD) fetch(g, gy, row);
-    for (int64_t first = (int64_t)blockIdx.x * slots; first < a.rows; first += stride, row += stride) {
-        float next_v[kAhead ? E : 1], next_g[kAhead && BWD ? E : 1];
-        if constexpr (kAhead) {
-            fetch(next_v, x, row + stride);
-            if constexpr (BWD) fetch(next_g, gy, row + stride);
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int j = 0; j < H; ++j) ones[j] = make_float2(inside(col(i) + 2 * j) ? 1.f : 0.f, inside(col(i) + 2 * j + 1) ? 1.f : 0.f);
+            w.r[i] = a.weight ? piecewise((const T*)a.weight, i) : P::from(ones);
+            b.r[i] = a.bias ? piecewise((const T*)a.bias, i) : P::none();
         }
-        float sum = 0.f, square = 0.f;
+    }
+
+    RowSum<LANES> row_sum{lanes, slot, 0, meet};
+    float2 sum_w[BWD ? E2 : 1], sum_b[BWD ? E2 : 1];
 #pragma unroll
-        for (int i = 0; i < E; ++i) sum += v[i];
-        const float mean = row_sum(make_float2(sum, 0.f)).x * a.inverse_n;
+    for (int k = 0; k < (BWD ? E2 : 1); ++k) sum_w[k] = sum_b[k] = make_float2(0.f, 0.f);
+    // the next row is on its way while one is worked on (two or three rows ahead: slower, 160 900 x 64 float32 forward 12.0 -> 14.9 us)
+    Part next_x, next_g;
+    fetch(next_x, x, row);
+    if constexpr (BWD) fetch(next_g, gy, row);
+    // All lanes of a block make the same number of turns (the shuffles need them): its first slot's row counts.
+    for (int64_t first = (int64_t)blockIdx.x * slots; first < a.rows; first += stride, row += stride) {
+        if (first >= real) {   // (the whole block's rows)
+            if (row < a.rows && out)
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+                for (int i = 0; i < NV; ++i) {
+                    T* const at = out + row * n + col(i);
+                    if (whole(i)) P::store(at, P::none());
+                    else if (RAGGED && col(i) < n)
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float d = col(i) < n ? v[i * V + j] - mean : 0.f;
-                v[i * V + j] = d;
-                square = fmaf(d, d, square);
+                        for (int j = 0; j < V; ++j)
+                            if (inside(col(i) + j)) at[j] = from_float<T>(0.f);
+                }
+            continue;
+        }
+        float2 v[E2], g[BWD ? E2 : 1];
+#pragma unroll
+        for (int k = 0; k < E2; ++k) {
+            v[k] = P::pair(next_x.r[k / H], k % H);
+            if constexpr (BWD) g[k] = P::pair(next_g.r[k / H], k % H);
+        }
+        if constexpr (RAGGED) {   // what an access took in from outside the row
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (!whole(i))
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        if (!inside(col(i) + j)) {
+                            (j & 1 ? v[i * H + j / 2].y : v[i * H + j / 2].x) = 0.f;
+                            if constexpr (BWD) (j & 1 ? g[i * H + j / 2].y : g[i * H + j / 2].x) = 0.f;
+                        }
+        }
+        fetch(next_x, x, row + stride);
+        if constexpr (BWD) fetch(next_g, gy, row + stride);
+        float2 sum = v[0];
+#pragma unroll
+        for (int k = 1; k < E2; ++k) sum = __fadd2_rn(sum, v[k]);
+        const float mean = row_sum(sum.x + sum.y) * a.inverse_n;
+        float2 square = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (whole(i)) {
+#pragma unroll
+                for (int j = 0; j < H; ++j) {
+                    v[i * H + j] = V == 1 ? make_float2(v[i * H].x - mean, 0.f) : __fadd2_rn(v[i * H + j], make_float2(-mean, -mean));
+                }
+            } else if (RAGGED) {   // (without, there is nothing but zeros here)
+#pragma unroll
+                for (int j = 0; j < H; ++j) {
+                    if (inside(col(i) + 2 * j)) v[i * H + j].x -= mean;
+                    if (inside(col(i) + 2 * j + 1)) v[i * H + j].y -= mean;
+                }
             }
-        // (the accurate root and division: twice a row)
-        const float inverse = 1.f / sqrtf(fmaf(row_sum(make_float2(square, 0.f)).x, a.inverse_n, a.eps));
-        float z[E];
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+            for (int j = 0; j < H; ++j) square = __ffma2_rn(v[i * H + j], v[i * H + j], square);
+        }
+        const float variance = row_sum(square.x + square.y) * a.inverse_n;
+        // (a padding row is zero throughout, also with eps = 0)
+        const float inverse = row < real ? rsqrtf(variance + a.eps) : 0.f;
+        const float2 inverse2 = make_float2(inverse, inverse);
+        float2 z[E2];
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                v[i * V + j] *= inverse;
-                const bool in = kKeep || col(i) < n;
-                z[i * V + j] = in ? fmaf(v[i * V + j], weight_at(i, j), bias_at(i, j)) : 0.f;
-            }
+        for (int k = 0; k < E2; ++k) {
+            v[k] = __fmul2_rn(v[k], inverse2);
+            z[k] = __ffma2_rn(v[k], P::pair(w.r[k / H], k % H), P::pair(b.r[k / H], k % H));
+        }
         if constexpr (!BWD) {
             activate(z, a.act);
         } else {
             times_slope(g, z, a.act);
-            float2 means = make_float2(0.f, 0.f);
+            float2 mean_u = make_float2(0.f, 0.f), mean_uv = mean_u;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int k = 0; k < E2; ++k) {   // (g is zero in padding rows and outside the row)
+                sum_b[k] = __fadd2_rn(sum_b[k], g[k]);
+                sum_w[k] = __ffma2_rn(g[k], v[k], sum_w[k]);
+                g[k] = __fmul2_rn(g[k], P::pair(w.r[k / H], k % H));
+                mean_u = __fadd2_rn(mean_u, g[k]);
+                mean_uv = __ffma2_rn(g[k], v[k], mean_uv);
+            }
+            const float2 means = row_sum(make_float2(mean_u.x + mean_u.y, mean_uv.x + mean_uv.y));
+            const float2 m0 = make_float2(-means.x * a.inverse_n, -means.x * a.inverse_n);
+            const float2 m1 = make_float2(-means.y * a.inverse_n, -means.y * a.inverse_n);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const int k = i * V + j;
-                    sum_b[k] += g[k];   // (zero in padding rows and behind the last column)
-                    sum_w[k] = fmaf(g[k], v[k], sum_w[k]);
-                    const bool in = kKeep || col(i) < n;
-                    g[k] *= in ? weight_at(i, j) : 0.f;
-                    means.x += g[k];
-                    means.y = fmaf(g[k], v[k], means.y);
-                }
-            means = row_sum(means);
-            means.x *= a.inverse_n;
-            means.y *= a.inverse_n;
-#pragma unroll
-            for (int k = 0; k < E; ++k) z[k] = (g[k] - fmaf(v[k], means.y, means.x)) * inverse;
+            for (int k = 0; k < E2; ++k) z[k] = __fmul2_rn(__fadd2_rn(g[k], __ffma2_rn(v[k], m1, m0)), inverse2);
         }
         if (row < a.rows && out) {
+            T* const at = out + row * n;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                float p[V];
+                float2 o[H];
 #pragma unroll
-                for (int j = 0; j < V; ++j) p[j] = row < real ? z[i * V + j] : 0.f;
-                if (col(i) < n) Pack<T, V>::store(out + row * n + col(i), p);
+                for (int j = 0; j < H; ++j) o[j] = z[i * H + j];
+                if (whole(i)) P::store(at + col(i), row < real ? P::from(o) : P::none());
+                else if (RAGGED && col(i) < n) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        if (inside(col(i) + j)) at[col(i) + j] = from_float<T>(row < real ? (j & 1 ? o[j / 2].y : o[j / 2].x) : 0.f);
+                }
             }
-        }
-        if constexpr (kAhead) {
-#pragma unroll
-            for (int i = 0; i < E; ++i) v[i] = next_v[i];
-            if constexpr (BWD)
-#pragma unroll
-                for (int i = 0; i < E; ++i) g[i] = next_g[i];
-        } else {
-            fetch(v, x, row + stride);
-            if constexpr (BWD) fetch(g, gy, row + stride);
         }
     }
     if constexpr (BWD) {
         if (!a.shares) return;
-        // the rows of a warp first, then the block's warps (or its slots of several warps) in order
-        if (lanes < 32)
+        // the rows of a warp first where they have the same columns, then what is left in order: a warp's slots, the block's warps
+        constexpr bool kTogether = !RAGGED && LANES > 0 && LANES < 32;
+        if constexpr (kTogether)
 #pragma unroll
-            for (int i = 0; i < E; ++i)
-                for (int o = 16; o >= lanes; o >>= 1) {
-                    sum_w[i] += __shfl_xor_sync(~0u, sum_w[i], o);
-                    sum_b[i] += __shfl_xor_sync(~0u, sum_b[i], o);
+            for (int k = 0; k < E2; ++k)
+#pragma unroll
+                for (int o = 16; o >= LANES; o >>= 1) {
+                    sum_w[k].x += __shfl_xor_sync(~0u, sum_w[k].x, o);
+                    sum_w[k].y += __shfl_xor_sync(~0u, sum_w[k].y, o);
+                    sum_b[k].x += __shfl_xor_sync(~0u, sum_b[k].x, o);
+                    sum_b[k].y += __shfl_xor_sync(~0u, sum_b[k].y, o);
                 }
-        const int turns = lanes <= 32 ? kNormWarps : slots, turn = lanes <= 32 ? (int)threadIdx.x >> 5 : slot;
-        const bool speaks = lanes >= 32 || (threadIdx.x & 31) < lanes;
-        for (int t = 0; t < turns; ++t) {
-            __syncthreads();   // (the first: nobody reads the parameters any more)
-            if (t == turn && speaks)
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int j = 0; j < V; ++j)
-                        if (col(i) < n) {
-                            float *pw = params + col(i) + j, *pb = pw + n;
-                            *pw = t == 0 ? sum_w[i * V + j] : *pw + sum_w[i * V + j];
-                            *pb = t == 0 ? sum_b[i * V + j] : *pb + sum_b[i * V + j];
-                        }
-        }
+        for (int i = threadIdx.x; i < 2 * n; i += kNormThreads) block_sums[i] = 0.f;
         __syncthreads();
+        const int turns = LANES ? kNormWarps : slots, turn = LANES ? (int)threadIdx.x >> 5 : slot;
+        const int per_warp = LANES > 0 && LANES < 32 && !kTogether ? 32 / lanes : 1;
+        for (int t = 0; t < turns; ++t) {
+            if (t == turn)
+                for (int s = 0; s < per_warp; ++s) {
+                    if (LANES == 0 || (int)(threadIdx.x & 31) / lanes == s)
+#pragma unroll
+                        for (int i = 0; i < NV; ++i)
+#pragma unroll
+                            for (int j = 0; j < V; ++j)
+                                if (inside(col(i) + j)) {
+                                    const float2 sw = sum_w[i * H + j / 2], sb = sum_b[i * H + j / 2];
+                                    block_sums[col(i) + j] += j & 1 ? sw.y : sw.x;
+                                    block_sums[n + col(i) + j] += j & 1 ? sb.y : sb.x;
+                                }
+                    __syncwarp();
+                }
+            __syncthreads();
+        }
         float* const to = a.shares + (int64_t)blockIdx.x * 2 * n;
-        for (int i = threadIdx.x; i < 2 * n; i += kNormThreads) to[i] = params[i];
+        for (int i = threadIdx.x; i < 2 * n; i += kNormThreads) to[i] = block_sums[i];
     }
 }
 
-// What a call runs on: V elements an access, NV accesses a lane, lanes a row.
-struct NormShape { int v, nv, lanes, blocks; };
+// What a call runs on.  16-byte accesses where the arrays start on 16 bytes, element by element elsewhere and in narrow rows that do
+// not (32 columns or fewer: little data, and sums slot by slot would take longer than the rows).
+struct NormShape { int vector, ragged, each, lanes, blocks; };
 
-// Elements a lane: up to 32 in the forward, up to 16 in the backward, which holds four such sets.
-NormShape norm_shape(int64_t rows, int n, int widest, bool bwd) {
+NormShape norm_shape(int64_t rows, int n, int size, bool bwd, bool aligned) {
     NormShape s{};
-    s.v = widest;
-    const int most = bwd ? 16 : 32;
-    const int pieces = (n + s.v - 1) / s.v;
+    const int v = 16 / size;
+    s.ragged = aligned && n % v != 0 && n > 32 && n + v - 1 <= 16 * kNormThreads;
+    s.vector = aligned && (n % v == 0 || s.ragged);
+    // Elements a lane: 8, or 16 in rows of more than 256 (fewer lanes to sum over) unless the backward's registers would not
+    // hold them, and whenever 8 are not enough.
+    const int width = n + (s.ragged ? v - 1 : 0);
+    s.each = width > 8 * kNormThreads || (width > 256 && (!bwd || (size == 2 && s.vector))) ? 16 : 8;
     s.lanes = 1;
-    while (s.lanes < 32 && s.lanes < pieces) s.lanes *= 2;
-    s.nv = 1;
-    while ((int64_t)s.lanes * s.nv < pieces) {
-        if (s.v * s.nv < most) s.nv *= 2;
-        else s.lanes *= 2;
-    }
+    while (s.lanes * s.each < width) s.lanes *= 2;
+    if (s.each == 16) s.lanes = std::max(s.lanes, 32);
     const int64_t per_turn = kNormThreads / s.lanes;
-    const int64_t resident = (int64_t)sm_count() * (s.v * s.nv <= 8 ? 4 : 2);
+    const int64_t resident = (int64_t)sm_count() * norm_blocks(s.vector ? v : 1, s.each, bwd);
     s.blocks = (int)std::min<int64_t>((rows + per_turn - 1) / per_turn, resident);
+    const int step = (int)std::max<int64_t>(v / per_turn, 1);   // (ragged rows: the stride is a multiple of v rows)
+    if (s.ragged) s.blocks = (s.blocks + step - 1) / step * step;
     return s;
 }
 
-// The widest access that every row's start allows.
-template <class T> int widest_access(int n, const void* const (&arrays)[3]) {
-    uintptr_t all = (uintptr_t)n * sizeof(T);
-    for (const void* p : arrays) all |= (uintptr_t)p;
-    if ((all & 15u) == 0) return 16 / (int)sizeof(T);
-    return sizeof(T) == 2 && (all & 3u) == 0 ? 2 : 1;
+template <class T, int V, int EACH, int LANES, bool RAGGED, bool BWD> int launch_norm(const NormArgs& a, const NormShape& s, cudaStream_t st) {
+    return launch_dependent(norm_kernel<T, V, EACH, LANES, RAGGED, BWD>, dim3((unsigned)s.blocks), dim3(kNormThreads),
+                            BWD ? sizeof(float) * 2 * (size_t)a.n : 0, st, a);
 }
-
-template <class T, int V, int NV, bool BWD> int launch_norm(const NormArgs& a, const NormShape& s, cudaStream_t st) {
-    return launch_dependent(norm_kernel<T, V, NV, BWD>, dim3((unsigned)s.blocks), dim3(kNormThreads),
-                            sizeof(float) * 2 * (size_t)a.n, st, a);
-}
-template <class T, int V, bool BWD> int launch_norm_nv(const NormArgs& a, const NormShape& s, cudaStream_t st) {
-    switch (s.nv) {
-        case 1: return launch_norm<T, V, 1, BWD>(a, s, st);
-        case 2: return launch_norm<T, V, 2, BWD>(a, s, st);
-        case 4: if constexpr (V * 4 <= (BWD ? 16 : 32)) return launch_norm<T, V, 4, BWD>(a, s, st); break;
-        case 8: if constexpr (V * 8 <= (BWD ? 16 : 32)) return launch_norm<T, V, 8, BWD>(a, s, st); break;
-        case 16: if constexpr (V * 16 <= (BWD ? 16 : 32)) return launch_norm<T, V, 16, BWD>(a, s, st); break;
-        case 32: if constexpr (V * 32 <= (BWD ? 16 : 32)) return launch_norm<T, V, 32, BWD>(a, s, st); break;
+template <class T, int V, bool RAGGED, bool BWD> int launch_norm_lanes(const NormArgs& a, const NormShape& s, cudaStream_t st) {
+    if (s.each == 16) return s.lanes == 32 ? launch_norm<T, V, 16, 32, RAGGED, BWD>(a, s, st) : launch_norm<T, V, 16, 0, RAGGED, BWD>(a, s, st);
+    if constexpr (!RAGGED) {   // (more than 32 columns: 4 lanes and more)
+        if (s.lanes == 1) return launch_norm<T, V, 8, 1, RAGGED, BWD>(a, s, st);
+        if (s.lanes == 2) return launch_norm<T, V, 8, 2, RAGGED, BWD>(a, s, st);
+        if (s.lanes == 4) return launch_norm<T, V, 8, 4, RAGGED, BWD>(a, s, st);
     }
-    return E3J_ERR_UNSUPPORTED;
+    if (s.lanes == 8) return launch_norm<T, V, 8, 8, RAGGED, BWD>(a, s, st);
+    if (s.lanes == 16) return launch_norm<T, V, 8, 16, RAGGED, BWD>(a, s, st);
+    if (s.lanes == 32) return launch_norm<T, V, 8, 32, RAGGED, BWD>(a, s, st);
+    return launch_norm<T, V, 8, 0, RAGGED, BWD>(a, s, st);
 }
 template <class T, bool BWD> int norm(NormArgs a, const NormShape& s, cudaStream_t st) {
     a.lanes = s.lanes;
-    if constexpr (sizeof(T) == 2) {
-        if (s.v == 8) return launch_norm_nv<T, 8, BWD>(a, s, st);
-        if (s.v == 2) return launch_norm_nv<T, 2, BWD>(a, s, st);
-    } else {
-        if (s.v == 4) return launch_norm_nv<T, 4, BWD>(a, s, st);
-    }
-    return launch_norm_nv<T, 1, BWD>(a, s, st);
+    constexpr int V = 16 / (int)sizeof(T);
+    if (s.ragged) return launch_norm_lanes<T, V, true, BWD>(a, s, st);
+    return s.vector ? launch_norm_lanes<T, V, false, BWD>(a, s, st) : launch_norm_lanes<T, 1, false, BWD>(a, s, st);
 }
+inline bool on_16_bytes(const void* p, const void* q, const void* r) { return (((uintptr_t)p | (uintptr_t)q | (uintptr_t)r) & 15u) == 0; }
 
 template <class T>
 int norm_fwd(NormArgs& a, cudaStream_t st) {
-    return norm<T, false>(a, norm_shape(a.rows, a.n, widest_access<T>(a.n, {a.x, a.out, nullptr}), false), st);
+    return norm<T, false>(a, norm_shape(a.rows, a.n, sizeof(T), false, on_16_bytes(a.x, a.out, nullptr)), st);
 }
 template <class T>
 int norm_bwd(NormArgs& a, void* grad_weight, void* grad_bias, cudaStream_t st) {
-    const NormShape s = norm_shape(a.rows, a.n, widest_access<T>(a.n, {a.x, a.grad_y, a.out}), true);
+    const NormShape s = norm_shape(a.rows, a.n, sizeof(T), true, on_16_bytes(a.x, a.grad_y, a.out));
     if (!grad_weight && !grad_bias) a.shares = nullptr;
     if (int rc = norm<T, true>(a, s, st)) return rc;
     if (!a.shares) return E3J_OK;
@@ -322,10 +376,10 @@ int e3j_layer_norm_fwd(int dtype, int64_t rows, int n, const void* x, const void
 
 size_t e3j_layer_norm_bwd_workspace_bytes(int dtype, int64_t rows, int n) {
     if (norm_args_status(rows, n, dtype, 0.0, E3J_ACT_NONE) != E3J_OK) return 0;
-    // (an access may be narrower than the width allows, where an array does not start on its boundary: more blocks)
-    size_t most = 0;
-    for (int v : {1, 2, 4, 8}) most = std::max(most, (size_t)norm_shape(rows, n, v, true).blocks);
-    return align_up(std::max<size_t>(most, 1) * 2 * n * sizeof(float), 256);
+    const int size = dtype == E3J_F32 ? 4 : 2;
+    size_t most = 1;   // (arrays that do not start on 16 bytes may have another number of blocks)
+    for (bool aligned : {false, true}) most = std::max<size_t>(most, norm_shape(rows, n, size, true, aligned).blocks);
+    return align_up(most * 2 * n * sizeof(float), 256);
 }
 
 int e3j_layer_norm_bwd(int dtype, int64_t rows, int n, const void* x, const void* weight, const void* bias, const void* grad_y,

@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(kLinThreads, LinTile<P, T, G, NT>::kBlocks) li
                                 const T* const at = (const T*)a.residual + row * width + f;
                                 if (whole && (a.vector & 8)) {
                                     float r[4];
-                                    Pack<T, 4>::load(r, at);
+                                    load_four(r, at);
 #pragma unroll
                                     for (int i = 0; i < 4; ++i) z[i] += r[i];
                                 } else {
@@ -374,16 +374,16 @@ __global__ void __launch_bounds__(kLinThreads, LinTile<P, T, G, NT>::kBlocks) li
                         if constexpr (P == kSlope) {
                             const T* const at = (const T*)a.grad_y + row * width + f;
                             float g[4];
-                            if (whole && (a.vector & 8)) Pack<T, 4>::load(g, at);
+                            if (whole && (a.vector & 8)) load_four(g, at);
                             else
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) g[i] = f + i < width ? to_float(at[i]) : 0.f;
                             times_slope(g, z, a.act);
                             // (rows of gz are padded to whole vectors)
-                            if (f < a.ld_gz) Pack<float, 4>::store((float*)a.out + row * a.ld_gz + f, g);
+                            if (f < a.ld_gz) store_four((float*)a.out + row * a.ld_gz + f, g);
                         } else {
                             T* const at = (T*)a.out + row * width + f;
-                            if (whole && (a.vector & 4)) Pack<T, 4>::store(at, z);
+                            if (whole && (a.vector & 4)) store_four(at, z);
                             else
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) if (f + i < width) at[i] = from_float<T>(z[i]);
