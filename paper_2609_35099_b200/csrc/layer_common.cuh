@@ -94,9 +94,20 @@ __device__ __forceinline__ void store_four(bf16* p, const float (&v)[4]) {
     *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
 }
 
-// 1 / (1 + exp(-z)).  The fast exponential and division are within a few float32 roundings where the result is not tiny;
-// exp(-z) = infinity gives 0.
-__device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+// 2^x and 1 / x by the hardware's approximations (within 2 and 1 steps of float32; results below the normal range are 0).
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float fast_reciprocal(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.44269504f;
+// 1 / (1 + exp(-z)); exp(-z) = infinity gives 0
+__device__ __forceinline__ float logistic(float z) { return fast_reciprocal(1.f + fast_exp2(-kLog2e * z)); }
 
 // Normal distribution: its density phi(z) and distribution function Phi(z) from one exponential.  erf by the rational approximation
 // of Hastings (Abramowitz and Stegun 7.1.26), 1 - (a1 t + .. + a5 t^5) exp(-x^2) with t = 1 / (1 + p x), which is within 1.5e-7
@@ -104,8 +115,8 @@ __device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f 
 // 49 157 rows of 385 bfloat16 with GELU is bound by instructions: backward NNN us, with erff MMM.
 __device__ __forceinline__ void normal(float z, float& phi, float& Phi) {
     const float x = fabsf(z) * 0.70710678f;
-    const float t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
-    const float e = __expf(-x * x);
+    const float t = fast_reciprocal(fmaf(0.3275911f, x, 1.f));
+    const float e = fast_exp2(-kLog2e * x * x);
     float poly = fmaf(1.061405429f, t, -1.453152027f);
     poly = fmaf(poly, t, 1.421413741f);
     poly = fmaf(poly, t, -0.284496736f);

@@ -23,62 +23,46 @@
 // of a 16-column group are dealt out so that the two pieces of a lane are four consecutive features: rows leave in 64-byte (float32) or
 // 32-byte (bfloat16) runs a quad, whole sectors, without a detour through shared memory.  (column_of)
 //
-// A block: 256 threads, all of which load, split and store operands and then read accumulators; thread 0 issues the tensor-core
-// instructions.  Two accumulator sets: while the tensor cores work on a tile, the block reads out the one before it and the loads
-// of the one after it are in flight; two blocks an SM fill each other's waits.  Waits are bounded (fast::mbar_wait).
+// A block is one per SM and has three roles: eight warps fetch, split and store operands (one chunk in registers ahead; bfloat16 rows
+// that start on 16 bytes go to shared memory by cp.async, up to four chunks ahead), one issues the tensor-core instructions, eight
+// read accumulators and finish tiles.  Operand stages and two accumulator sets stand between them.  As one role of 256 threads
+// that took turns, two blocks an SM, the same instructions took NNN.  Waits are bounded (fast::mbar_wait).
 #pragma once
 #include "layer_common.cuh"
+#include "linear.hpp"
 #include "umma.cuh"
 
 namespace e3j {
 namespace layer {
 
-constexpr int kLinThreads = 256;
+constexpr int kRoleThreads = 256;   // of the loaders, and of the readers
+constexpr int kLinThreads = 2 * kRoleThreads + 32;
+constexpr int kMostStages = 6;
 constexpr int kTileRows = 128;      // accumulator lanes
 constexpr int kChunk = 64;          // contraction elements a chunk
 constexpr int kGroupChunks = 4;     // chunks a chain (float32 sums over rows)
 constexpr int kPanelBytes = 64 * 128;   // 64 rows of a panel
-
-enum Product { kForward, kSlope, kGradX, kGradW };
-// kForward  y = act(x W + b) + residual
-// kSlope    gz = grad_y act'(x W + b), float32, into the workspace
-// kGradX    grad_x = gz W^T
-// kGradW    shares of x^T gz and of the column sums of gz, one a range of rows
-
-struct LinArgs {
-    int64_t rows;
-    int n_in, n_out, act;
-    const int32_t* n_real;
-    const void *x, *W, *b, *residual, *grad_y;
-    const void* gz;        // kGradX, kGradW: grad_y itself where there is no activation
-    int ld_gz;             // elements between its rows
-    void* out;
-    float* shares;         // kGradW: [ranges][n_in * n_out + n_out]
-    int ranges, want_sums;
-    int n_tiles;           // tiles of 128 (kGradW: of its two dimensions, n_tiles x m_tiles) or NT columns
-    int m_tiles;
-    int stages, resident;  // operand stages; B's chunks stay in shared memory
-    unsigned vector;       // which arrays' rows start on 16 bytes: bit 0 A, 1 B, 2 out, 3 residual / grad_y
-    int32_t* status;
-};
 
 // ---------------------------------------------------------------- operands
 template <class T> struct Piece;   // 8 elements as they lie in memory
 template <> struct Piece<float> { float v[8]; };
 template <> struct Piece<bf16> { uint32_t v[4]; };
 
-__device__ __forceinline__ void load_piece(Piece<float>& p, const float* from, int left, bool vector) {
-    if (left >= 8 && vector) {
-        const float4 a = __ldg(reinterpret_cast<const float4*>(from)), b = __ldg(reinterpret_cast<const float4*>(from) + 1);
+// `left` elements of the row are there (0 or less: none), the rest is zero.  VEC: rows start on 16 bytes and are whole 16-byte pieces.
+template <bool VEC> __device__ __forceinline__ void load_piece(Piece<float>& p, const float* from, int left) {
+    if constexpr (VEC) {
+        const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float4 a = left >= 4 ? __ldg(reinterpret_cast<const float4*>(from)) : none;
+        const float4 b = left >= 8 ? __ldg(reinterpret_cast<const float4*>(from) + 1) : none;
         p.v[0] = a.x; p.v[1] = a.y; p.v[2] = a.z; p.v[3] = a.w; p.v[4] = b.x; p.v[5] = b.y; p.v[6] = b.z; p.v[7] = b.w;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) p.v[i] = i < left ? __ldg(from + i) : 0.f;
     }
 }
-__device__ __forceinline__ void load_piece(Piece<bf16>& p, const bf16* from, int left, bool vector) {
-    if (left >= 8 && vector) {
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>(from));
+template <bool VEC> __device__ __forceinline__ void load_piece(Piece<bf16>& p, const bf16* from, int left) {
+    if constexpr (VEC) {
+        const uint4 a = left >= 8 ? __ldg(reinterpret_cast<const uint4*>(from)) : make_uint4(0, 0, 0, 0);
         p.v[0] = a.x; p.v[1] = a.y; p.v[2] = a.z; p.v[3] = a.w;
     } else {
         const uint16_t* const h = reinterpret_cast<const uint16_t*>(from);
@@ -87,14 +71,58 @@ __device__ __forceinline__ void load_piece(Piece<bf16>& p, const bf16* from, int
             p.v[i] = (2 * i < left ? (uint32_t)__ldg(h + 2 * i) : 0u) | (2 * i + 1 < left ? (uint32_t)__ldg(h + 2 * i + 1) << 16 : 0u);
     }
 }
+// Four consecutive elements, `left` of which are there, as they lie in memory.
+template <class T> struct Quad;
+template <> struct Quad<float> {
+    float4 q;
+    __device__ __forceinline__ void add_to(float (&v)[4]) const { v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w; }
+};
+template <> struct Quad<bf16> {
+    uint2 q;
+    __device__ __forceinline__ void add_to(float (&v)[4]) const {
+        v[0] += low_float(q.x); v[1] += high_float(q.x); v[2] += low_float(q.y); v[3] += high_float(q.y);
+    }
+};
+template <bool VEC> __device__ __forceinline__ void load_quad(Quad<float>& v, const float* from, int left) {
+    v.q = make_float4(0.f, 0.f, 0.f, 0.f);
+    if constexpr (VEC) {
+        if (left >= 4) v.q = __ldg(reinterpret_cast<const float4*>(from));
+    } else {
+        if (left > 0) v.q.x = __ldg(from);
+        if (left > 1) v.q.y = __ldg(from + 1);
+        if (left > 2) v.q.z = __ldg(from + 2);
+        if (left > 3) v.q.w = __ldg(from + 3);
+    }
+}
+template <bool VEC> __device__ __forceinline__ void load_quad(Quad<bf16>& v, const bf16* from, int left) {
+    v.q = make_uint2(0, 0);
+    if constexpr (VEC) {
+        if (left >= 4) v.q = __ldg(reinterpret_cast<const uint2*>(from));
+    } else {
+        const uint16_t* const h = reinterpret_cast<const uint16_t*>(from);
+        if (left > 0) v.q.x = __ldg(h);
+        if (left > 1) v.q.x |= (uint32_t)__ldg(h + 1) << 16;
+        if (left > 2) v.q.y = __ldg(h + 2);
+        if (left > 3) v.q.y |= (uint32_t)__ldg(h + 3) << 16;
+    }
+}
+template <bool VEC, class T> __device__ __forceinline__ void store_quad(T* to, const float (&v)[4], int left) {
+    if constexpr (VEC) {
+        if (left >= 4) store_four(to, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) if (i < left) to[i] = from_float<T>(v[i]);
+    }
+}
 __device__ __forceinline__ float element(const Piece<float>& p, int i) { return p.v[i]; }
 __device__ __forceinline__ float element(const Piece<bf16>& p, int i) { return i & 1 ? high_float(p.v[i / 2]) : low_float(p.v[i / 2]); }
 
 // The terms of a piece, packed in pairs.
 __device__ __forceinline__ uint32_t cut_pair(float& a, float& b) {   // the leading 8 bits of both; what is left in a, b
     const uint32_t p = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
-    a -= low_float(p);
-    b -= high_float(p);
+    const float2 left = __fadd2_rn(make_float2(a, b), make_float2(-low_float(p), -high_float(p)));
+    a = left.x;
+    b = left.y;
     return p;
 }
 template <int TERMS> __device__ __forceinline__ void split(const Piece<float>& p, uint32_t (&t)[TERMS][4]) {
@@ -147,34 +175,35 @@ __device__ __forceinline__ void tmem_ld_quads(uint32_t taddr, float (&v)[8]) {
 
 // Operand block of ROWS rows and COLS columns, taken in pieces of 8 columns (8 or 16 a row), or in pairs of pieces of 16 columns whose
 // order inside the group is column_of's (PERMUTED columns).
-template <class T, int TERMS, int ROWS, int COLS, bool PAIRS> struct Operand {
+template <class T, int TERMS, int ROWS, int COLS, bool PAIRS, bool VEC> struct Operand {
     static constexpr int kWide = PAIRS ? 16 : 8;
     static constexpr int kAcross = COLS / kWide;
-    static constexpr int kItems = ROWS * kAcross / kLinThreads;
+    static constexpr int kItems = ROWS * kAcross / kRoleThreads;
     static constexpr uint32_t kTermBytes = ROWS * COLS * 2;
     static constexpr uint32_t kBytes = TERMS * kTermBytes;
-    static_assert(ROWS * kAcross % kLinThreads == 0, "the threads share the items");
+    static_assert(ROWS * kAcross % kRoleThreads == 0, "the threads share the items");
     Piece<T> p[kItems][PAIRS ? 2 : 1];
 
     // rows [row0, row_end) and columns [col0, col_end) of `from` are there, the rest is zero
-    __device__ __forceinline__ void load(const T* from, int64_t ld, int64_t row0, int64_t row_end, int col0, int col_end, bool vector) {
+    // (t: this thread among the loaders)
+    __device__ __forceinline__ void load(int t, const T* from, int64_t ld, int64_t row0, int64_t row_end, int col0, int col_end) {
+        const int row = t / kAcross, col = col0 + t % kAcross * kWide;
+        const int rows = (int)min(row_end - row0, (int64_t)ROWS);
+        const T* at = from + (row0 + row) * ld + col;
+        const int64_t step = ld * (kRoleThreads / kAcross);
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            const int item = i * kLinThreads + threadIdx.x;
-            const int64_t row = row0 + item / kAcross;
-            const int col = col0 + item % kAcross * kWide;
-            const T* const at = from + row * ld + col;
-            const int left = row < row_end ? col_end - col : 0;
-            load_piece(p[i][0], at, left, vector);
-            if constexpr (PAIRS) load_piece(p[i][1], at + 8, left - 8, vector);
+        for (int i = 0; i < kItems; ++i, at += step) {
+            const int left = row + i * (kRoleThreads / kAcross) < rows ? col_end - col : 0;
+            load_piece<VEC>(p[i][0], at, left);
+            if constexpr (PAIRS) load_piece<VEC>(p[i][1], at + 8, left - 8);
         }
     }
     // PERMUTE_ROWS: the block's rows become the tile's columns
     template <bool PERMUTE_ROWS = false>
-    __device__ __forceinline__ void store(unsigned char* image) const {
+    __device__ __forceinline__ void store(int thread, unsigned char* image) const {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            const int item = i * kLinThreads + threadIdx.x;
+            const int item = i * kRoleThreads + thread;
             int row = item / kAcross;
             const int across = item % kAcross;
             if constexpr (PERMUTE_ROWS) row = column_of(row);
@@ -200,6 +229,33 @@ template <class T, int TERMS, int ROWS, int COLS, bool PAIRS> struct Operand {
     }
 };
 
+// The same block straight into shared memory (one term, rows that start on 16 bytes): 16-byte pieces, zeros where nothing is.
+template <int ROWS, int COLS>
+__device__ __forceinline__ void copy_async(int t, uint32_t image, const bf16* from, int64_t ld, int64_t row0, int64_t row_end,
+                                           int col0, int col_end) {
+    constexpr int kAcross = COLS / 8, kItems = ROWS * kAcross / kRoleThreads, kRows = kRoleThreads / kAcross;
+    const int row = t / kAcross, across = t % kAcross, col = col0 + across * 8;
+    const int rows = col < col_end ? (int)min(row_end - row0, (int64_t)ROWS) : 0;
+    const bf16* at = from + (row0 + row) * ld + col;
+    const int64_t step = ld * kRows;
+    static_assert(kRows % 8 == 0, "an item's place in the swizzle is the same for all items");
+    const uint32_t to = image + (across >> 3) * (ROWS * 128) + image_offset(row, across & 7);
+#pragma unroll
+    for (int i = 0; i < kItems; ++i, at += step) {
+        const bool there = row + i * kRows < rows;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + i * kRows * 128), "l"(there ? at : from),
+                     "r"(there ? 16 : 0) : "memory");
+    }
+}
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// all but the newest `n` groups have arrived
+__device__ __forceinline__ void async_wait(int n) {
+    if (n >= 3) asm volatile("cp.async.wait_group 3;" ::: "memory");
+    else if (n == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else if (n == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
 // ---------------------------------------------------------------- the kernel
 // T: type of the layer's tensors; G: type of gz (kGradX, kGradW).
 template <Product P, class T, class G> struct Types {
@@ -215,54 +271,59 @@ template <class T, class G> struct Types<kGradW, T, G> {
     static constexpr int a_terms = sizeof(T) == 4 ? 3 : 1, b_terms = sizeof(G) == 2 ? 1 : sizeof(T) == 4 ? 3 : 2;
 };
 
-template <Product P, class T, class G, int NT> struct LinTile {
+template <Product P, class T, class G, int NT, bool VEC> struct LinTile {
     using Ty = Types<P, T, G>;
     static constexpr bool kRowSum = P == kGradW;    // contraction over rows: both operands MN-major
-    using OpA = Operand<typename Ty::A, Ty::a_terms, kRowSum ? kChunk : kTileRows, kRowSum ? kTileRows : kChunk, false>;
-    using OpB = Operand<typename Ty::B, Ty::b_terms, P == kGradX ? NT : kChunk, P == kGradX ? kChunk : NT, P != kGradX>;
+    using OpA = Operand<typename Ty::A, Ty::a_terms, kRowSum ? kChunk : kTileRows, kRowSum ? kTileRows : kChunk, false, VEC>;
+    using OpB = Operand<typename Ty::B, Ty::b_terms, P == kGradX ? NT : kChunk, P == kGradX ? kChunk : NT, P != kGradX, VEC>;
     static constexpr bool kA_mn = kRowSum, kB_mn = P != kGradX;
     static constexpr int kSets = Ty::a_terms == 3 ? 2 : 1;     // accumulators of a tile
     static constexpr int kColumns = 2 * kSets * NT;            // tensor memory: two tiles
-    static constexpr int kBlocks = kColumns <= 256 ? 2 : 1;    // blocks an SM
+    static constexpr bool kAsyncA = VEC && sizeof(typename Ty::A) == 2;   // A by cp.async
     static size_t smem_bytes(int stages, int b_slots) { return 1024 + (size_t)stages * OpA::kBytes + (size_t)b_slots * OpB::kBytes; }
 };
 
-template <Product P, class T, class G, int NT>
-__global__ void __launch_bounds__(kLinThreads, LinTile<P, T, G, NT>::kBlocks) linear_kernel(const __grid_constant__ LinArgs a) {
-    using L = LinTile<P, T, G, NT>;
+template <Product P, class T, class G, int NT, int ACT, bool VEC>
+__global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_constant__ LinArgs a) {
+    using L = LinTile<P, T, G, NT, VEC>;
     using TA = typename L::Ty::A;
     using TB = typename L::Ty::B;
     using OpA = typename L::OpA;
     using OpB = typename L::OpB;
     constexpr int kTermsA = L::Ty::a_terms, kTermsB = L::Ty::b_terms;
     extern __shared__ unsigned char raw_smem[];
-    __shared__ uint64_t stage_free[2], tile_done[2], drain;
+    __shared__ uint64_t full[kMostStages], empty[kMostStages], tile_full[2], tile_empty[2], drain;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word, drain_word;
     __shared__ float column_sums[P == kGradW ? 16 * NT : 1];
-    __shared__ float bias[P == kForward || P == kSlope ? NT : 1];
+    __shared__ __align__(16) float bias[P == kForward || P == kSlope ? NT : 4];
     unsigned char* const smem = raw_smem + ((1024u - (umma::smem_addr(raw_smem) & 1023u)) & 1023u);
     volatile int* const abort_flag = &abort_word;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int kRoleWarps = kRoleThreads / 32;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 2; ++i) { fast::mbar_init(&stage_free[i], 1); fast::mbar_init(&tile_done[i], 1); }
+        for (int i = 0; i < kMostStages; ++i) { fast::mbar_init(&full[i], kRoleWarps); fast::mbar_init(&empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { fast::mbar_init(&tile_full[i], 1); fast::mbar_init(&tile_empty[i], kRoleWarps); }
         fast::mbar_init(&drain, 1);
         abort_word = drain_word = 0;
         fast::mbar_fence_init();
     }
-    if (warp == 0) umma::tmem_alloc(&tmem_slot, L::kColumns);
+    if (warp == 2 * kRoleWarps) umma::tmem_alloc(&tmem_slot, L::kColumns);
+    fast::grid_dependency_wait();
+    fast::grid_dependency_trigger();
+    const int nt = blockIdx.x % a.n_tiles;
+    const int n0 = nt * NT;
+    if constexpr (P == kForward || P == kSlope)
+        if (threadIdx.x < NT)
+            bias[threadIdx.x] = a.b && n0 + (int)threadIdx.x < a.n_out ? to_float(((const T*)a.b)[n0 + threadIdx.x]) : 0.f;
     umma::fence_before_sync();
     __syncthreads();
     umma::fence_after_sync();
     const uint32_t tmem = tmem_slot;
-    fast::grid_dependency_wait();
-    fast::grid_dependency_trigger();
     const int64_t real = real_rows(a.rows, a.n_real);
 
     // ---- what this block does: units (a tile, or for kGradW a group of chunks of one tile) of `chunks` chunks
-    const int nt = blockIdx.x % a.n_tiles;
-    const int n0 = nt * NT;
     int units, chunks, m0 = 0;
     int64_t unit0 = 0, unit_step = 1;          // row tiles of this block
     int64_t chunk_begin = 0, chunk_end = 0;    // kGradW: chunks of rows of this block
@@ -285,250 +346,268 @@ __global__ void __launch_bounds__(kLinThreads, LinTile<P, T, G, NT>::kBlocks) li
         if constexpr (P == kGradW) return (int)min((int64_t)kGroupChunks, chunk_end - chunk_begin - (int64_t)unit * kGroupChunks);
         else return chunks;
     };
-
-    OpA op_a;
-    OpB op_b;
-    auto load_a = [&](int unit, int chunk) {
-        const bool vec = a.vector & 1;
-        if constexpr (P == kGradW) {
-            const int64_t row0 = (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunk;
-            op_a.load((const TA*)a.x, a.n_in, row0, real, m0, a.n_in, vec);
-        } else {
-            const int64_t row0 = (unit0 + unit * unit_step) * kTileRows;
-            if constexpr (P == kGradX) op_a.load((const TA*)a.gz, a.ld_gz, row0, real, chunk * kChunk, a.n_out, vec);
-            else op_a.load((const TA*)a.x, a.n_in, row0, real, chunk * kChunk, a.n_in, vec);
-        }
-    };
-    auto load_b = [&](int unit, int chunk) {
-        const bool vec = a.vector & 2;
-        if constexpr (P == kGradW) {
-            const int64_t row0 = (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunk;
-            op_b.load((const TB*)a.gz, a.ld_gz, row0, real, n0, a.n_out, vec);
-        } else if constexpr (P == kGradX) {
-            op_b.load((const TB*)a.W, a.n_out, n0, a.n_in, chunk * kChunk, a.n_out, vec);
-        } else {
-            op_b.load((const TB*)a.W, a.n_out, chunk * kChunk, a.n_in, n0, a.n_out, vec);
-        }
-    };
     unsigned char* const b_area = smem + (size_t)a.stages * OpA::kBytes;
 
-    if constexpr (P == kForward || P == kSlope)
-        if (threadIdx.x < NT)
-            bias[threadIdx.x] = a.b && n0 + (int)threadIdx.x < a.n_out ? to_float(((const T*)a.b)[n0 + threadIdx.x]) : 0.f;
-
-    // ---- accumulators -> registers -> memory
-    const int half = warp >> 2, quarter = warp & 3;
-    float sums[P == kGradW ? NT / 2 : 1];
+    if (warp >= kRoleWarps && warp < 2 * kRoleWarps) {
+        // ------------------------------------------------ loaders: memory -> terms -> stages
+        const int t = threadIdx.x - kRoleThreads;
+        OpA op_a;
+        OpB op_b;
+        auto with_a = [&](int unit, int chunk, auto&& f) {   // the block of A that a chunk takes
+            if constexpr (P == kGradW) f((const TA*)a.x, (int64_t)a.n_in, (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunk, m0, a.n_in);
+            else if constexpr (P == kGradX) f((const TA*)a.gz, (int64_t)a.ld_gz, (unit0 + unit * unit_step) * kTileRows, chunk * kChunk, a.ld_gz);
+            else f((const TA*)a.x, (int64_t)a.n_in, (unit0 + unit * unit_step) * kTileRows, chunk * kChunk, a.n_in);
+        };
+        auto load_a = [&](int unit, int chunk) {
+            if constexpr (!L::kAsyncA)
+                with_a(unit, chunk, [&](const TA* from, int64_t ld, int64_t row0, int col0, int col_end) { op_a.load(t, from, ld, row0, real, col0, col_end); });
+        };
+        auto load_b = [&](int unit, int chunk) {
+            if constexpr (P == kGradW) op_b.load(t, (const TB*)a.gz, a.ld_gz, (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunk, real, n0, a.ld_gz);
+            else if constexpr (P == kGradX) op_b.load(t, (const TB*)a.W, a.n_out, n0, a.n_in, chunk * kChunk, a.n_out);
+            else op_b.load(t, (const TB*)a.W, a.n_out, chunk * kChunk, a.n_in, n0, a.n_out);
+        };
+        float col_sum[P == kGradW ? 16 : 1];
 #pragma unroll
-    for (int i = 0; i < (P == kGradW ? NT / 2 : 1); ++i) sums[i] = 0.f;
-    auto read_out = [&](int unit, int set) {
-#pragma unroll
-        for (int c = 0; c < NT / 2; c += 16) {
-            const int col = half * (NT / 2) + c;              // of the tile
-            const int f = n0 + col + 4 * (lane & 3);          // first of this lane's four features
-            if (P != kGradW && n0 + col >= (P == kGradX ? a.n_in : a.n_out)) break;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {                     // 16 of the warp's 32 lanes of tensor memory
-                const uint32_t taddr = tmem + ((uint32_t)(quarter * 32 + h * 16) << 16) + (uint32_t)(set * L::kSets * NT + col);
-                float v[8];
-                __syncwarp();
-                tmem_ld_quads(taddr, v);
-                if constexpr (L::kSets == 2) {
-                    float u[8];
-                    tmem_ld_quads(taddr + NT, u);
-                    umma::tmem_ld_wait();
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] += u[i];
-                } else {
-                    umma::tmem_ld_wait();
+        for (int i = 0; i < (P == kGradW ? 16 : 1); ++i) col_sum[i] = 0.f;
+        if (units > 0) {
+            load_a(0, 0);
+            if (!a.resident) load_b(0, 0);
+            else
+                for (int k = 0; k < chunks; ++k) {
+                    load_b(0, k);
+                    op_b.template store<P == kGradX>(t, b_area + (size_t)k * OpB::kBytes);
                 }
-                if constexpr (P == kGradW) {
+        }
+        const int lag = L::kAsyncA ? min(a.stages - 1, 3) : 0;   // chunks of cp.async on their way behind the newest
+        int stage = 0, late = 0, unreported = 0;
+        uint32_t turn = 0;
+        bool ok = true;
+        auto report = [&] {   // the oldest stage that has not been handed over
+            umma::fence_smem_to_async();
+            __syncwarp();
+            if (lane == 0) fast::mbar_arrive(&full[late]);
+            late = late + 1 == a.stages ? 0 : late + 1;
+            --unreported;
+        };
+        for (int unit = 0; ok && unit < units; ++unit) {
+            const int n_chunks = chunks_of(unit);
+            for (int chunk = 0; chunk < n_chunks; ++chunk) {
+                if (turn > 0 && !(ok = fast::mbar_wait(&empty[stage], (turn - 1) & 1, abort_flag, a.status))) break;
+                unsigned char* const to = smem + (size_t)stage * OpA::kBytes;
+                if constexpr (L::kAsyncA)
+                    with_a(unit, chunk, [&](const TA* from, int64_t ld, int64_t row0, int col0, int col_end) {
+                        copy_async<P == kGradW ? kChunk : kTileRows, P == kGradW ? kTileRows : kChunk>(t, umma::smem_addr(to), from, ld, row0, real, col0, col_end);
+                    });
+                else op_a.store(t, to);
+                if (!a.resident) {
+                    op_b.template store<P == kGradX>(t, b_area + (size_t)stage * OpB::kBytes);
+                    if constexpr (P == kGradW) {
+                        if (a.want_sums && m0 == 0) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sums[(c / 16 * 2 + h) * 8 + i] += v[i];
-                } else {
+                            for (int i = 0; i < OpB::kItems; ++i)
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const int64_t row = (unit0 + unit * unit_step) * kTileRows + quarter * 32 + h * 16 + s * 8 + lane / 4;
-                        float z[4] = {v[2 * s], v[2 * s + 1], v[4 + 2 * s], v[5 + 2 * s]};
-                        if constexpr (P == kForward || P == kSlope)
+                                for (int j = 0; j < 16; ++j) col_sum[j] += element(op_b.p[i][j >> 3], j & 7);
+                        }
+                    }
+                }
+                if constexpr (L::kAsyncA) async_commit();
+                if (++unreported > lag) {
+                    if constexpr (L::kAsyncA) async_wait(lag);
+                    report();
+                }
+                const bool more = chunk + 1 < n_chunks;
+                if (more || unit + 1 < units) {
+                    load_a(more ? unit : unit + 1, more ? chunk + 1 : 0);
+                    if (!a.resident) load_b(more ? unit : unit + 1, more ? chunk + 1 : 0);
+                }
+                if (++stage == a.stages) { stage = 0; ++turn; }
+            }
+        }
+        if constexpr (L::kAsyncA) async_wait(0);
+        while (ok && unreported > 0) report();
+        if constexpr (P == kGradW) {
+            if (a.want_sums && m0 == 0) {
+                // a thread's 16 columns are the same in every chunk; groups of threads in turn, 16 at a time
+                constexpr int kAcross = OpB::kAcross, kGroups = kRoleThreads / kAcross;
+                static_assert(kGroups % 16 == 0, "");
+                const int across = t % kAcross, group = t / kAcross;
+                for (int s = 0; s < kGroups / 16; ++s) {
+                    if (group / 16 == s)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) z[i] += bias[col + 4 * (lane & 3) + i];
-                        if (row >= real) continue;
-                        const int width = P == kGradX ? a.n_in : a.n_out;
-                        const bool whole = f + 4 <= width;
-                        if constexpr (P == kForward) {
-                            activate(z, a.act);
-                            if (a.residual) {
-                                const T* const at = (const T*)a.residual + row * width + f;
-                                if (whole && (a.vector & 8)) {
-                                    float r[4];
-                                    load_four(r, at);
+                        for (int j = 0; j < 16; ++j) {
+                            float* const at = &column_sums[(group % 16) * NT + across * 16 + j];
+                            *at = s == 0 ? col_sum[j] : *at + col_sum[j];
+                        }
+                    asm volatile("bar.sync 1, %0;" ::"n"(kRoleThreads) : "memory");
+                }
+                if (t < NT && n0 + t < a.n_out) {
+                    float sum = 0.f;
+                    for (int r = 0; r < 16; ++r) sum += column_sums[r * NT + t];
+                    const int range = blockIdx.x / (a.n_tiles * a.m_tiles);
+                    a.shares[(size_t)(range + 1) * ((size_t)a.n_in * a.n_out + a.n_out) - a.n_out + n0 + t] = sum;
+                }
+            }
+        } else if (P != kSlope && real < a.rows) {
+            // zero rows behind the last real one
+            const int width = P == kGradX ? a.n_in : a.n_out;
+            T* const out = (T*)a.out;
+            for (int64_t i = real * width + blockIdx.x * (int64_t)kRoleThreads + t; i < a.rows * width; i += (int64_t)gridDim.x * kRoleThreads)
+                out[i] = from_float<T>(0.f);
+        }
+    } else if (warp == 2 * kRoleWarps) {
+        // ------------------------------------------------ tensor cores
+        if (lane == 0) {
+            const uint32_t a_addr = umma::smem_addr(smem), b_addr = umma::smem_addr(b_area);
+            constexpr uint32_t a_step = L::kA_mn ? 2048 : 32, b_step = L::kB_mn ? 2048 : 32;
+            constexpr uint32_t one = idesc_bf16(kTileRows, NT, L::kA_mn, L::kB_mn);
+            constexpr uint32_t two = idesc_bf16(kTileRows, 2 * NT <= 256 ? 2 * NT : NT, L::kA_mn, L::kB_mn);
+            int stage = 0;
+            uint32_t turn = 0;
+            bool ok = true;
+            for (int unit = 0; ok && unit < units; ++unit) {
+                const int n_chunks = chunks_of(unit);
+                const int set = unit & 1;
+                if (unit >= 2 && !(ok = fast::mbar_wait(&tile_empty[set], ((unit >> 1) - 1) & 1, abort_flag, a.status))) break;
+                const uint32_t d = tmem + (uint32_t)(set * L::kSets * NT);
+                for (int chunk = 0; chunk < n_chunks; ++chunk) {
+                    if (!(ok = fast::mbar_wait(&full[stage], turn & 1, abort_flag, a.status))) break;
+                    umma::fence_after_sync();
+                    const uint32_t pa = a_addr + stage * OpA::kBytes, pb = b_addr + (a.resident ? chunk : stage) * OpB::kBytes;
+                    int steps = kChunk / 16;   // those that hold anything
+                    if constexpr (P != kGradW) steps = min(steps, ((P == kGradX ? a.n_out : a.n_in) - chunk * kChunk + 15) / 16);
+                    for (int k = 0; k < steps; ++k) {
+                        const uint32_t add = chunk > 0 || k > 0;   // (else the accumulators are overwritten)
+                        auto da = [&](int term) { return swizzled_desc(pa + term * OpA::kTermBytes + k * a_step, kPanelBytes, 1024); };
+                        auto db = [&](int term) { return swizzled_desc(pb + term * OpB::kTermBytes + k * b_step, kPanelBytes, 1024); };
+                        if constexpr (kTermsA == 3) {
+                            mma_bf16(d, da(0), db(0), two, add);         // hi [hi | mid]
+                            mma_bf16(d + NT, da(1), db(0), one, 1);
+                            mma_bf16(d + NT, da(1), db(1), one, 1);
+                            mma_bf16(d + NT, da(0), db(2), one, 1);
+                            mma_bf16(d + NT, da(2), db(0), one, 1);
+                        } else {
+                            mma_bf16(d, da(0), db(0), one, add);
+                            if constexpr (kTermsA == 2) mma_bf16(d, da(1), db(0), one, 1);
+                            if constexpr (kTermsB == 2) mma_bf16(d, da(0), db(1), one, 1);
+                        }
+                    }
+                    umma::commit(&empty[stage]);
+                    if (++stage == a.stages) { stage = 0; ++turn; }
+                }
+                if (ok) umma::commit(&tile_full[set]);
+            }
+            // everything issued is over before tensor memory goes back, also after a wait that ran out
+            umma::commit(&drain);
+            fast::mbar_wait(&drain, 0, &drain_word, a.status);
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------ readers: accumulators -> registers -> memory
+        const int half = warp >> 2, quarter = warp & 3;
+        float sums[P == kGradW ? NT / 2 : 1];
 #pragma unroll
-                                    for (int i = 0; i < 4; ++i) z[i] += r[i];
-                                } else {
+        for (int i = 0; i < (P == kGradW ? NT / 2 : 1); ++i) sums[i] = 0.f;
+        // What the results meet in memory, residual or grad_y, is fetched before the tile is waited for: kSlots groups of 16 columns
+        // (as many as the registers hold), the others as these become free.
+        constexpr bool kMeets = P == kForward || P == kSlope;
+        constexpr int kGroups = NT / 32, kSlots = !kMeets ? 1 : sizeof(T) == 4 ? 2 : kGroups;
+        Quad<T> meets[kSlots][2][2];
+        const int width = P == kGradX ? a.n_in : a.n_out;
+        const int f0 = n0 + half * (NT / 2) + 4 * (lane & 3);     // first of this lane's four features in the first group
+        const T* const meet = (const T*)(P == kForward ? a.residual : a.grad_y);
+        for (int unit = 0; unit < units; ++unit) {
+            const int set = unit & 1;
+            const int64_t row0 = (unit0 + unit * unit_step) * kTileRows + quarter * 32 + lane / 4;
+            auto fetch = [&](int c) {
+                if constexpr (kMeets)
 #pragma unroll
-                                    for (int i = 0; i < 4; ++i) if (f + i < width) z[i] += to_float(at[i]);
-                                }
+                    for (int r = 0; r < 4; ++r)
+                        load_quad<VEC>(meets[c % kSlots][r >> 1][r & 1], meet + (row0 + 8 * r) * width + f0 + 16 * c,
+                                       row0 + 8 * r < real ? width - f0 - 16 * c : 0);
+            };
+            if (kMeets && meet)
+#pragma unroll
+                for (int c = 0; c < kSlots; ++c) fetch(c);
+            if (!fast::mbar_wait(&tile_full[set], (unit >> 1) & 1, abort_flag, a.status)) break;
+            umma::fence_after_sync();
+#pragma unroll
+            for (int c = 0; c < kGroups; ++c) {
+                const int col = half * (NT / 2) + 16 * c;         // of the tile
+                const int f = f0 + 16 * c;
+                if (P != kGradW && n0 + col >= width) break;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {                     // 16 of the warp's 32 lanes of tensor memory
+                    const uint32_t taddr = tmem + ((uint32_t)(quarter * 32 + h * 16) << 16) + (uint32_t)(set * L::kSets * NT + col);
+                    float v[8];
+                    __syncwarp();
+                    tmem_ld_quads(taddr, v);
+                    if constexpr (L::kSets == 2) {
+                        float u[8];
+                        tmem_ld_quads(taddr + NT, u);
+                        umma::tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 8; i += 2) {
+                            const float2 w = __fadd2_rn(make_float2(v[i], v[i + 1]), make_float2(u[i], u[i + 1]));
+                            v[i] = w.x;
+                            v[i + 1] = w.y;
+                        }
+                    } else {
+                        umma::tmem_ld_wait();
+                    }
+                    if constexpr (P == kGradW) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) sums[(c * 2 + h) * 8 + i] += v[i];
+                    } else {
+#pragma unroll
+                        for (int s = 0; s < 2; ++s) {
+                            const int64_t row = row0 + h * 16 + s * 8;
+                            float z[4] = {v[2 * s], v[2 * s + 1], v[4 + 2 * s], v[5 + 2 * s]};
+                            if constexpr (kMeets) {
+                                const float4 b = *reinterpret_cast<const float4*>(bias + col + 4 * (lane & 3));
+                                z[0] += b.x; z[1] += b.y; z[2] += b.z; z[3] += b.w;
+                            }
+                            if (row >= real) continue;
+                            if constexpr (P == kForward) {
+                                activate_as<ACT>(z);
+                                if (meet) meets[c % kSlots][h][s].add_to(z);
+                            }
+                            if constexpr (P == kSlope) {
+                                float g[4] = {0.f, 0.f, 0.f, 0.f};
+                                meets[c % kSlots][h][s].add_to(g);
+                                times_slope_as<ACT>(g, z);
+                                store_quad<true>((float*)a.out + row * a.ld_gz + f, g, a.ld_gz - f);   // (whole vectors: ld_gz)
+                            } else {
+                                store_quad<VEC>((T*)a.out + row * width + f, z, width - f);
                             }
                         }
-                        if constexpr (P == kSlope) {
-                            const T* const at = (const T*)a.grad_y + row * width + f;
-                            float g[4];
-                            if (whole && (a.vector & 8)) load_four(g, at);
-                            else
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) g[i] = f + i < width ? to_float(at[i]) : 0.f;
-                            times_slope(g, z, a.act);
-                            // (rows of gz are padded to whole vectors)
-                            if (f < a.ld_gz) store_four((float*)a.out + row * a.ld_gz + f, g);
-                        } else {
-                            T* const at = (T*)a.out + row * width + f;
-                            if (whole && (a.vector & 4)) store_four(at, z);
-                            else
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) if (f + i < width) at[i] = from_float<T>(z[i]);
-                        }
                     }
                 }
+                if (kMeets && meet && c + kSlots < kGroups) fetch(c + kSlots);
             }
-        }
-        umma::fence_before_sync();
-    };
-
-    // ---- the pipeline
-    float col_sum[P == kGradW ? 16 : 1];
-#pragma unroll
-    for (int i = 0; i < (P == kGradW ? 16 : 1); ++i) col_sum[i] = 0.f;
-    const uint32_t a_addr = umma::smem_addr(smem), b_addr = umma::smem_addr(b_area);
-    uint32_t step = 0;   // chunks so far
-    if (units > 0) {
-        if (a.resident)
-            for (int k = 0; k < chunks; ++k) {
-                load_b(0, k);
-                op_b.template store<P == kGradX>(b_area + (size_t)k * OpB::kBytes);
-            }
-        else load_b(0, 0);
-        load_a(0, 0);
-    }
-    for (int unit = 0; unit < units; ++unit) {
-        const int n_chunks = chunks_of(unit);
-        const int set = unit & 1;
-        for (int chunk = 0; chunk < n_chunks; ++chunk, ++step) {
-            const int stage = a.stages == 2 ? step & 1 : 0;
-            const int b_slot = a.resident ? chunk : stage;
-            if (step >= (uint32_t)a.stages)   // the products that read this stage last are over
-                fast::mbar_wait(&stage_free[stage], ((step / a.stages) - 1) & 1, abort_flag, a.status);
-            op_a.store(smem + (size_t)stage * OpA::kBytes);
-            if (!a.resident) {
-                op_b.template store<P == kGradX>(b_area + (size_t)stage * OpB::kBytes);
-                if constexpr (P == kGradW) {
-                    if (a.want_sums && m0 == 0) {
-#pragma unroll
-                        for (int i = 0; i < OpB::kItems; ++i)
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) col_sum[j] += element(op_b.p[i][j >> 3], j & 7);
-                    }
-                }
-            }
-            umma::fence_smem_to_async();
             umma::fence_before_sync();
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                umma::fence_after_sync();
-                const uint32_t d = tmem + (uint32_t)(set * L::kSets * NT);
-                const uint32_t pa = a_addr + stage * OpA::kBytes, pb = b_addr + b_slot * OpB::kBytes;
-                constexpr uint32_t a_step = L::kA_mn ? 2048 : 32, b_step = L::kB_mn ? 2048 : 32;
-                constexpr uint32_t one = idesc_bf16(kTileRows, NT, L::kA_mn, L::kB_mn);
-                constexpr uint32_t two = idesc_bf16(kTileRows, 2 * NT, L::kA_mn, L::kB_mn);
-                // k-steps that hold anything
-                int steps = kChunk / 16;
-                if constexpr (P != kGradW) steps = min(steps, ((P == kGradX ? a.n_out : a.n_in) - chunk * kChunk + 15) / 16);
-                for (int k = 0; k < steps; ++k) {
-                    const uint32_t add = chunk > 0 || k > 0;   // (else the accumulators are overwritten)
-                    auto da = [&](int term) { return swizzled_desc(pa + term * OpA::kTermBytes + k * a_step, kPanelBytes, 1024); };
-                    auto db = [&](int term) { return swizzled_desc(pb + term * OpB::kTermBytes + k * b_step, kPanelBytes, 1024); };
-                    if constexpr (kTermsA == 3) {
-                        mma_bf16(d, da(0), db(0), two, add);         // hi [hi | mid]
-                        mma_bf16(d + NT, da(1), db(0), one, 1);
-                        mma_bf16(d + NT, da(1), db(1), one, 1);
-                        mma_bf16(d + NT, da(0), db(2), one, 1);
-                        mma_bf16(d + NT, da(2), db(0), one, 1);
-                    } else {
-                        mma_bf16(d, da(0), db(0), one, add);
-                        if constexpr (kTermsA == 2) mma_bf16(d, da(1), db(0), one, 1);
-                        if constexpr (kTermsB == 2) mma_bf16(d, da(0), db(1), one, 1);
-                    }
-                }
-                umma::commit(&stage_free[stage]);
-                if (chunk + 1 == n_chunks) umma::commit(&tile_done[set]);
-            }
-            const bool more = chunk + 1 < n_chunks;
-            if (more || unit + 1 < units) {
-                load_a(more ? unit : unit + 1, more ? chunk + 1 : 0);
-                if (!a.resident) load_b(more ? unit : unit + 1, more ? chunk + 1 : 0);
-            }
-            if (chunk == 0 && unit > 0) {   // the tile before this one
-                fast::mbar_wait(&tile_done[set ^ 1], ((unit - 1) >> 1) & 1, abort_flag, a.status);
-                umma::fence_after_sync();
-                read_out(unit - 1, set ^ 1);
-            }
+            __syncwarp();
+            if (lane == 0) fast::mbar_arrive(&tile_empty[set]);
         }
-    }
-    if (units > 0) {
-        fast::mbar_wait(&tile_done[(units - 1) & 1], ((units - 1) >> 1) & 1, abort_flag, a.status);
-        umma::fence_after_sync();
-        read_out(units - 1, (units - 1) & 1);
-    }
-
-    if constexpr (P == kGradW) {
-        const int range = blockIdx.x / (a.n_tiles * a.m_tiles);
-        float* const share = a.shares + (size_t)range * ((size_t)a.n_in * a.n_out + a.n_out);
+        if constexpr (P == kGradW) {
+            const int range = blockIdx.x / (a.n_tiles * a.m_tiles);
+            float* const share = a.shares + (size_t)range * ((size_t)a.n_in * a.n_out + a.n_out);
 #pragma unroll
-        for (int c = 0; c < NT / 2; c += 16)
+            for (int c = 0; c < NT / 2; c += 16)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int row = m0 + quarter * 32 + h * 16 + ((i >> 1) & 1) * 8 + lane / 4;
-                    const int f = n0 + half * (NT / 2) + c + 4 * (lane & 3) + (i & 1) + ((i >> 2) << 1);
-                    if (row < a.n_in && f < a.n_out) share[(size_t)row * a.n_out + f] = sums[(c / 16 * 2 + h) * 8 + i];
-                }
-        if (a.want_sums && m0 == 0) {
-            // a thread's 16 columns are the same in every chunk: [16 or more row groups][NT]
-            constexpr int kAcross = OpB::kAcross, kGroups = kLinThreads / kAcross;
-            static_assert(kGroups == 32 || kGroups == 64, "");
-            const int across = threadIdx.x % kAcross, group = threadIdx.x / kAcross;
-            // groups of threads in turn, 16 at a time
-            for (int t = 0; t < kGroups / 16; ++t) {
-                if (group / 16 == t)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        float* const at = &column_sums[(group % 16) * NT + across * 16 + j];
-                        *at = t == 0 ? col_sum[j] : *at + col_sum[j];
+                    for (int i = 0; i < 8; ++i) {
+                        const int row = m0 + quarter * 32 + h * 16 + ((i >> 1) & 1) * 8 + lane / 4;
+                        const int f = n0 + half * (NT / 2) + c + 4 * (lane & 3) + (i & 1) + ((i >> 2) << 1);
+                        if (row < a.n_in && f < a.n_out) share[(size_t)row * a.n_out + f] = sums[(c / 16 * 2 + h) * 8 + i];
                     }
-                __syncthreads();
-            }
-            if (threadIdx.x < NT && n0 + (int)threadIdx.x < a.n_out) {
-                float s = 0.f;
-                for (int r = 0; r < 16; ++r) s += column_sums[r * NT + threadIdx.x];
-                share[(size_t)a.n_in * a.n_out + n0 + threadIdx.x] = s;
-            }
         }
-    } else if (P != kSlope && real < a.rows) {
-        // zero rows behind the last real one
-        const int width = P == kGradX ? a.n_in : a.n_out;
-        T* const out = (T*)a.out;
-        for (int64_t i = real * width + blockIdx.x * (int64_t)kLinThreads + threadIdx.x; i < a.rows * width; i += (int64_t)gridDim.x * kLinThreads)
-            out[i] = from_float<T>(0.f);
-    }
-    if (threadIdx.x == 0 && *abort_flag) {   // a wait ran out: the tensor cores finish before tensor memory goes back
-        umma::commit(&drain);
-        fast::mbar_wait(&drain, 0, &drain_word, a.status);
     }
     umma::fence_before_sync();
     __syncthreads();
     umma::fence_after_sync();
-    if (warp == 0) umma::tmem_dealloc(tmem, L::kColumns);
+    if (warp == 2 * kRoleWarps) umma::tmem_dealloc(tmem, L::kColumns);
 }
 
 }  // namespace layer

@@ -1,0 +1,109 @@
+// Launches of linear_kernels.cuh for one type of the layer's tensors: included by linear_f32.cu and linear_bf16.cu.
+#pragma once
+#include <algorithm>
+#include <atomic>
+
+#include "linear.hpp"
+#include "linear_kernels.cuh"
+
+namespace e3j {
+namespace layer {
+
+constexpr size_t kSmemOfBlock = 227 * 1024;
+
+template <Product P, class T, class G, int NT, int ACT, bool VEC>
+struct Launch {
+    using L = LinTile<P, T, G, NT, VEC>;
+    static constexpr auto kernel = linear_kernel<P, T, G, NT, ACT, VEC>;
+    static constexpr size_t kStatic = (P == kGradW ? 16 * NT : NT) * sizeof(float) + 512;
+    // Operand stages, and whether all of B's chunks stay in shared memory (with two stages at least).
+    static int shape(LinArgs& a, int chunks, size_t& smem) {
+        for (int resident = P == kGradW ? 0 : 1; resident >= 0; --resident)
+            for (int stages = kMostStages; stages >= 2; --stages) {
+                smem = L::smem_bytes(stages, resident ? chunks : stages);
+                if (smem > kSmemOfBlock - kStatic) continue;
+                a.stages = stages;
+                a.resident = resident;
+                return E3J_OK;
+            }
+        return E3J_ERR_UNSUPPORTED;   // (never: two stages of every kind fit)
+    }
+    static int run(LinArgs& a, cudaStream_t st) {
+        static std::atomic<uint64_t> allowed{0};   // bit per device
+        int dev = 0;
+        E3J_CUDA_TRY(cudaGetDevice(&dev));
+        if (dev < 0 || dev >= 64) return E3J_ERR_UNSUPPORTED;
+        if (!(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
+            E3J_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmemOfBlock - kStatic)));
+            allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
+        }
+        const int columns = P == kGradX ? a.n_in : a.n_out;
+        a.n_tiles = (columns + NT - 1) / NT;
+        size_t smem = 0;
+        if (int rc = shape(a, ((P == kGradX ? a.n_out : a.n_in) + kChunk - 1) / kChunk, smem)) return rc;
+        int64_t grid;
+        if (P == kGradW) {
+            grid = (int64_t)a.n_tiles * a.m_tiles * a.ranges;
+        } else {
+            const int64_t row_tiles = (a.rows + kTileRows - 1) / kTileRows;
+            const int64_t per = std::max<int64_t>(sm_count() / a.n_tiles, 1);
+            grid = a.n_tiles * std::min(per, row_tiles);
+        }
+        return launch_dependent(kernel, dim3((unsigned)grid), dim3(kLinThreads), smem, st, a);
+    }
+};
+
+template <Product P, class T, class G, int ACT = E3J_ACT_NONE> int product(LinArgs& a, bool vector, cudaStream_t st) {
+    const bool narrow = (P == kGradX ? a.n_in : a.n_out) <= 64;
+    if (vector) return narrow ? Launch<P, T, G, 64, ACT, true>::run(a, st) : Launch<P, T, G, 128, ACT, true>::run(a, st);
+    return narrow ? Launch<P, T, G, 64, ACT, false>::run(a, st) : Launch<P, T, G, 128, ACT, false>::run(a, st);
+}
+template <Product P, class T, class G> int product_act(LinArgs& a, int act, bool vector, cudaStream_t st) {
+    if (act == E3J_ACT_SILU) return product<P, T, G, E3J_ACT_SILU>(a, vector, st);
+    if (act == E3J_ACT_TANH) return product<P, T, G, E3J_ACT_TANH>(a, vector, st);
+    if (act == E3J_ACT_GELU) return product<P, T, G, E3J_ACT_GELU>(a, vector, st);
+    if constexpr (P == kForward) return product<P, T, G>(a, vector, st);
+    return E3J_ERR_INVALID_ARG;
+}
+
+// Rows of `ld` elements from p on start on 16 bytes and are whole 16-byte pieces (p null: so they do).
+inline bool whole(const void* p, int64_t ld, size_t size) { return !p || (((uintptr_t)p | (uintptr_t)(ld * size)) & 15u) == 0; }
+
+template <class T> int linear_fwd(LinArgs& a, int act, cudaStream_t st) {
+    const bool vector = whole(a.x, a.n_in, sizeof(T)) && whole(a.W, a.n_out, sizeof(T)) && whole(a.out, a.n_out, sizeof(T)) &&
+                        whole(a.residual, a.n_out, sizeof(T));
+    return product_act<kForward, T, T>(a, act, vector, st);
+}
+
+template <class T, class G> int gradients(LinArgs a, const BwdLayout& L, void* grad_x, void* grad_W, void* grad_b, cudaStream_t st) {
+    const bool gz = whole(a.gz, a.ld_gz, sizeof(G));
+    if (grad_x) {
+        a.out = grad_x;
+        if (int rc = product<kGradX, T, G>(a, gz && whole(a.W, a.n_out, sizeof(T)) && whole(grad_x, a.n_in, sizeof(T)), st)) return rc;
+    }
+    if (!grad_W && !grad_b) return E3J_OK;
+    a.ranges = L.ranges;
+    a.m_tiles = L.m_tiles;
+    a.want_sums = grad_b != nullptr;
+    if (int rc = product<kGradW, T, G>(a, gz && whole(a.x, a.n_in, sizeof(T)), st)) return rc;
+    return sum_shares<T>(L.ranges, (int64_t)a.n_in * a.n_out, a.n_out, a.shares, (T*)grad_W, (T*)grad_b, st);
+}
+
+template <class T>
+int linear_bwd(LinArgs& a, int act, const BwdLayout& L, void* workspace, void* grad_x, void* grad_W, void* grad_b, cudaStream_t st) {
+    a.shares = (float*)((char*)workspace + L.shares);
+    if (act == E3J_ACT_NONE) {
+        a.gz = a.grad_y;
+        a.ld_gz = a.n_out;
+        return gradients<T, T>(a, L, grad_x, grad_W, grad_b, st);
+    }
+    a.out = workspace;
+    a.ld_gz = (int)L.ld_gz;
+    const bool vector = whole(a.x, a.n_in, sizeof(T)) && whole(a.W, a.n_out, sizeof(T)) && whole(a.grad_y, a.n_out, sizeof(T));
+    if (int rc = product_act<kSlope, T, float>(a, act, vector, st)) return rc;
+    a.gz = workspace;
+    return gradients<T, float>(a, L, grad_x, grad_W, grad_b, st);
+}
+
+}  // namespace layer
+}  // namespace e3j
