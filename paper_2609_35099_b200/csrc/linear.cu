@@ -38,8 +38,15 @@ int status_word(int32_t** word) {
     return E3J_OK;
 }
 
-BwdLayout bwd_layout(int64_t rows, int n_in, int n_out, int act) {
+BwdLayout bwd_layout(int dtype, int64_t rows, int n_in, int n_out, int act) {
     BwdLayout L{};
+    const size_t share = ((size_t)n_in * n_out + n_out) * sizeof(float);
+    L.narrow = n_in <= 64 && n_out <= 64;
+    if (L.narrow) {
+        L.ranges = (int)std::min<int64_t>(std::max<int64_t>((rows + 127) / 128, 1), sm_count());
+        L.total = align_up(L.ranges * (dtype == E3J_F32 ? 2 : 1) * share, 256);   // (float32: two shares a block)
+        return L;
+    }
     L.ld_gz = align_up(n_out, 8);
     const int nt = n_out <= 64 ? 64 : 128;
     const int n_tiles = (n_out + nt - 1) / nt;
@@ -48,7 +55,7 @@ BwdLayout bwd_layout(int64_t rows, int n_in, int n_out, int act) {
     const int64_t resident = sm_count();
     L.ranges = (int)std::min(std::max<int64_t>(resident / (n_tiles * L.m_tiles), 1), chunks);
     L.shares = act == E3J_ACT_NONE ? 0 : align_up((size_t)rows * L.ld_gz * sizeof(float), 256);
-    L.total = L.shares + align_up((size_t)L.ranges * ((size_t)n_in * n_out + n_out) * sizeof(float), 256);
+    L.total = L.shares + align_up(L.ranges * share, 256);
     return L;
 }
 
@@ -83,7 +90,7 @@ int e3j_linear_fwd(int dtype, int64_t rows, int n_in, int n_out, const void* x, 
 
 size_t e3j_linear_bwd_workspace_bytes(int dtype, int64_t rows, int n_in, int n_out, int act) {
     if (linear_args_status(dtype, rows, n_in, n_out, act) != E3J_OK) return 0;
-    return bwd_layout(rows, n_in, n_out, act).total;
+    return bwd_layout(dtype, rows, n_in, n_out, act).total;
 }
 
 int e3j_linear_bwd(int dtype, int64_t rows, int n_in, int n_out, const void* x, const void* W, const void* b, const void* grad_y,
@@ -102,7 +109,7 @@ int e3j_linear_bwd(int dtype, int64_t rows, int n_in, int n_out, const void* x, 
     }
     if (!x || !W || !grad_y) return E3J_ERR_INVALID_ARG;
     if (!grad_x && !grad_W && !grad_b) return E3J_OK;
-    const BwdLayout L = bwd_layout(rows, n_in, n_out, act);
+    const BwdLayout L = bwd_layout(dtype, rows, n_in, n_out, act);
     if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < L.total) return E3J_ERR_WORKSPACE;
     LinArgs a{};
     a.rows = rows; a.n_in = n_in; a.n_out = n_out; a.n_real = n_real;

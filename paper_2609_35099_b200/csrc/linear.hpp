@@ -30,8 +30,9 @@ struct LinArgs {
     int32_t* status;
 };
 
-// The backward's workspace: [gz | shares].
-struct BwdLayout { int64_t ld_gz; int m_tiles, ranges; size_t shares, total; };
+// The backward: one sweep where both widths are at most 64, else three products with gz in memory.  Workspace: [gz | shares];
+// ranges: the rows' division (narrow: blocks of the sweep).
+struct BwdLayout { bool narrow; int64_t ld_gz; int m_tiles, ranges; size_t shares, total; };
 
 // Calls with rows > 0 and checked arguments; T: float or __nv_bfloat16.
 template <class T> int linear_fwd(LinArgs& a, int act, cudaStream_t st);

@@ -162,6 +162,12 @@ __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uin
         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
+// The other way round: into tensor memory.
+__device__ __forceinline__ void tmem_st_quads(uint32_t taddr, const float (&v)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(taddr), "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])),
+                   "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])) : "memory");
+}
 // 16 lanes x 16 columns: v[0], v[1], v[4], v[5] are row lane / 4, the others row lane / 4 + 8; columns 2 (lane % 4) and the next one, of
 // the first and of the second 8.
 __device__ __forceinline__ void tmem_ld_quads(uint32_t taddr, float (&v)[8]) {
@@ -175,13 +181,13 @@ __device__ __forceinline__ void tmem_ld_quads(uint32_t taddr, float (&v)[8]) {
 
 // Operand block of ROWS rows and COLS columns, taken in pieces of 8 columns (8 or 16 a row), or in pairs of pieces of 16 columns whose
 // order inside the group is column_of's (PERMUTED columns).
-template <class T, int TERMS, int ROWS, int COLS, bool PAIRS, bool VEC> struct Operand {
+template <class T, int TERMS, int ROWS, int COLS, bool PAIRS, bool VEC, int THREADS = kRoleThreads> struct Operand {
     static constexpr int kWide = PAIRS ? 16 : 8;
     static constexpr int kAcross = COLS / kWide;
-    static constexpr int kItems = ROWS * kAcross / kRoleThreads;
+    static constexpr int kItems = ROWS * kAcross / THREADS;
     static constexpr uint32_t kTermBytes = ROWS * COLS * 2;
     static constexpr uint32_t kBytes = TERMS * kTermBytes;
-    static_assert(ROWS * kAcross % kRoleThreads == 0, "the threads share the items");
+    static_assert(ROWS * kAcross % THREADS == 0, "the threads share the items");
     Piece<T> p[kItems][PAIRS ? 2 : 1];
 
     // rows [row0, row_end) and columns [col0, col_end) of `from` are there, the rest is zero
@@ -190,10 +196,10 @@ template <class T, int TERMS, int ROWS, int COLS, bool PAIRS, bool VEC> struct O
         const int row = t / kAcross, col = col0 + t % kAcross * kWide;
         const int rows = (int)min(row_end - row0, (int64_t)ROWS);
         const T* at = from + (row0 + row) * ld + col;
-        const int64_t step = ld * (kRoleThreads / kAcross);
+        const int64_t step = ld * (THREADS / kAcross);
 #pragma unroll
         for (int i = 0; i < kItems; ++i, at += step) {
-            const int left = row + i * (kRoleThreads / kAcross) < rows ? col_end - col : 0;
+            const int left = row + i * (THREADS / kAcross) < rows ? col_end - col : 0;
             load_piece<VEC>(p[i][0], at, left);
             if constexpr (PAIRS) load_piece<VEC>(p[i][1], at + 8, left - 8);
         }
@@ -203,7 +209,7 @@ template <class T, int TERMS, int ROWS, int COLS, bool PAIRS, bool VEC> struct O
     __device__ __forceinline__ void store(int thread, unsigned char* image) const {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            const int item = i * kRoleThreads + thread;
+            const int item = i * THREADS + thread;
             int row = item / kAcross;
             const int across = item % kAcross;
             if constexpr (PERMUTE_ROWS) row = column_of(row);

@@ -4,12 +4,25 @@
 #include <atomic>
 
 #include "linear.hpp"
+#include "linear_bwd_narrow.cuh"
 #include "linear_kernels.cuh"
 
 namespace e3j {
 namespace layer {
 
 constexpr size_t kSmemOfBlock = 227 * 1024;
+
+// Lets a kernel have that much dynamic shared memory on the current device (once: a bit per device).
+template <class K> int allow_smem(K kernel, size_t bytes, std::atomic<uint64_t>& allowed) {
+    int dev = 0;
+    E3J_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return E3J_ERR_UNSUPPORTED;
+    if (!(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
+        E3J_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+        allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
+    return E3J_OK;
+}
 
 template <Product P, class T, class G, int NT, int ACT, bool VEC>
 struct Launch {
@@ -29,14 +42,8 @@ struct Launch {
         return E3J_ERR_UNSUPPORTED;   // (never: two stages of every kind fit)
     }
     static int run(LinArgs& a, cudaStream_t st) {
-        static std::atomic<uint64_t> allowed{0};   // bit per device
-        int dev = 0;
-        E3J_CUDA_TRY(cudaGetDevice(&dev));
-        if (dev < 0 || dev >= 64) return E3J_ERR_UNSUPPORTED;
-        if (!(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
-            E3J_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmemOfBlock - kStatic)));
-            allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
-        }
+        static std::atomic<uint64_t> allowed{0};
+        if (int rc = allow_smem(kernel, kSmemOfBlock - kStatic, allowed)) return rc;
         const int columns = P == kGradX ? a.n_in : a.n_out;
         a.n_tiles = (columns + NT - 1) / NT;
         size_t smem = 0;
@@ -89,9 +96,32 @@ template <class T, class G> int gradients(LinArgs a, const BwdLayout& L, void* g
     return sum_shares<T>(L.ranges, (int64_t)a.n_in * a.n_out, a.n_out, a.shares, (T*)grad_W, (T*)grad_b, st);
 }
 
+template <class T, int ACT, bool VEC> int narrow_kernel(LinArgs& a, int blocks, cudaStream_t st) {
+    using S = NarrowLayout<T, ACT>;
+    constexpr auto kernel = linear_bwd_narrow_kernel<T, ACT, VEC>;
+    static std::atomic<uint64_t> allowed{0};
+    if (int rc = allow_smem(kernel, S::smem, allowed)) return rc;
+    return launch_dependent(kernel, dim3((unsigned)blocks), dim3(kNarrowThreads), S::smem, st, a);
+}
+template <class T, int ACT> int narrow_bwd(LinArgs& a, const BwdLayout& L, void* grad_W, void* grad_b, cudaStream_t st) {
+    const bool vector = whole(a.x, a.n_in, sizeof(T)) && whole(a.W, a.n_out, sizeof(T)) && whole(a.grad_y, a.n_out, sizeof(T)) &&
+                        whole(a.out, a.n_in, sizeof(T));
+    if (!grad_W && !grad_b) a.shares = nullptr;
+    if (int rc = vector ? narrow_kernel<T, ACT, true>(a, L.ranges, st) : narrow_kernel<T, ACT, false>(a, L.ranges, st)) return rc;
+    if (!a.shares) return E3J_OK;
+    return sum_shares<T>(L.ranges * NarrowLayout<T, ACT>::parts, (int64_t)a.n_in * a.n_out, a.n_out, a.shares, (T*)grad_W, (T*)grad_b, st);
+}
+
 template <class T>
 int linear_bwd(LinArgs& a, int act, const BwdLayout& L, void* workspace, void* grad_x, void* grad_W, void* grad_b, cudaStream_t st) {
     a.shares = (float*)((char*)workspace + L.shares);
+    if (L.narrow) {
+        a.out = grad_x;
+        if (act == E3J_ACT_SILU) return narrow_bwd<T, E3J_ACT_SILU>(a, L, grad_W, grad_b, st);
+        if (act == E3J_ACT_TANH) return narrow_bwd<T, E3J_ACT_TANH>(a, L, grad_W, grad_b, st);
+        if (act == E3J_ACT_GELU) return narrow_bwd<T, E3J_ACT_GELU>(a, L, grad_W, grad_b, st);
+        return narrow_bwd<T, E3J_ACT_NONE>(a, L, grad_W, grad_b, st);
+    }
     if (act == E3J_ACT_NONE) {
         a.gz = a.grad_y;
         a.ld_gz = a.n_out;
