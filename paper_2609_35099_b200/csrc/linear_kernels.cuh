@@ -44,33 +44,6 @@ constexpr int kGroupChunks = 4;     // chunks a chain (float32 sums over rows)
 constexpr int kPanelBytes = 64 * 128;   // 64 rows of a panel
 
 // ---------------------------------------------------------------- operands
-template <class T> struct Piece;   // 8 elements as they lie in memory
-template <> struct Piece<float> { float v[8]; };
-template <> struct Piece<bf16> { uint32_t v[4]; };
-
-// `left` elements of the row are there (0 or less: none), the rest is zero.  VEC: rows start on 16 bytes and are whole 16-byte pieces.
-template <bool VEC> __device__ __forceinline__ void load_piece(Piece<float>& p, const float* from, int left) {
-    if constexpr (VEC) {
-        const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
-        const float4 a = left >= 4 ? __ldg(reinterpret_cast<const float4*>(from)) : none;
-        const float4 b = left >= 8 ? __ldg(reinterpret_cast<const float4*>(from) + 1) : none;
-        p.v[0] = a.x; p.v[1] = a.y; p.v[2] = a.z; p.v[3] = a.w; p.v[4] = b.x; p.v[5] = b.y; p.v[6] = b.z; p.v[7] = b.w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p.v[i] = i < left ? __ldg(from + i) : 0.f;
-    }
-}
-template <bool VEC> __device__ __forceinline__ void load_piece(Piece<bf16>& p, const bf16* from, int left) {
-    if constexpr (VEC) {
-        const uint4 a = left >= 8 ? __ldg(reinterpret_cast<const uint4*>(from)) : make_uint4(0, 0, 0, 0);
-        p.v[0] = a.x; p.v[1] = a.y; p.v[2] = a.z; p.v[3] = a.w;
-    } else {
-        const uint16_t* const h = reinterpret_cast<const uint16_t*>(from);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            p.v[i] = (2 * i < left ? (uint32_t)__ldg(h + 2 * i) : 0u) | (2 * i + 1 < left ? (uint32_t)__ldg(h + 2 * i + 1) << 16 : 0u);
-    }
-}
 // Four consecutive elements, `left` of which are there, as they lie in memory.
 template <class T> struct Quad;
 template <> struct Quad<float> {
@@ -114,30 +87,27 @@ template <bool VEC, class T> __device__ __forceinline__ void store_quad(T* to, c
         for (int i = 0; i < 4; ++i) if (i < left) to[i] = from_float<T>(v[i]);
     }
 }
-__device__ __forceinline__ float element(const Piece<float>& p, int i) { return p.v[i]; }
-__device__ __forceinline__ float element(const Piece<bf16>& p, int i) { return i & 1 ? high_float(p.v[i / 2]) : low_float(p.v[i / 2]); }
-
-// The terms of a piece, packed in pairs.
-__device__ __forceinline__ uint32_t cut_pair(float& a, float& b) {   // the leading 8 bits of both; what is left in a, b
+// Cuts the leading 8 bits off two values: a term of both, packed; what is left of them in a, b.
+__device__ __forceinline__ uint32_t cut_pair(float& a, float& b) {
     const uint32_t p = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
     const float2 left = __fadd2_rn(make_float2(a, b), make_float2(-low_float(p), -high_float(p)));
     a = left.x;
     b = left.y;
     return p;
 }
-template <int TERMS> __device__ __forceinline__ void split(const Piece<float>& p, uint32_t (&t)[TERMS][4]) {
+// The terms of four elements, packed in pairs; the last is rounded (of three it is exact).
+template <int TERMS> __device__ __forceinline__ void split(const Quad<float>& v, uint2 (&t)[TERMS]) {
+    float a = v.q.x, b = v.q.y, c = v.q.z, d = v.q.w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float a = p.v[2 * i], b = p.v[2 * i + 1];
-#pragma unroll
-        for (int k = 0; k + 1 < TERMS; ++k) t[k][i] = cut_pair(a, b);
-        t[TERMS - 1][i] = pack_bf16(a, b);   // (exact as the third of three)
+    for (int k = 0; k + 1 < TERMS; ++k) {
+        t[k].x = cut_pair(a, b);
+        t[k].y = cut_pair(c, d);
     }
+    t[TERMS - 1] = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
 }
-template <int TERMS> __device__ __forceinline__ void split(const Piece<bf16>& p, uint32_t (&t)[TERMS][4]) {
+template <int TERMS> __device__ __forceinline__ void split(const Quad<bf16>& v, uint2 (&t)[TERMS]) {
     static_assert(TERMS == 1, "bfloat16 is one term");
-#pragma unroll
-    for (int i = 0; i < 4; ++i) t[0][i] = p.v[i];
+    t[0] = v.q;
 }
 
 __device__ __forceinline__ uint32_t image_offset(int row, int piece) { return (uint32_t)(row * 128 + ((piece ^ (row & 7)) << 4)); }
@@ -179,56 +149,46 @@ __device__ __forceinline__ void tmem_ld_quads(uint32_t taddr, float (&v)[8]) {
     for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-// Operand block of ROWS rows and COLS columns, taken in pieces of 8 columns (8 or 16 a row), or in pairs of pieces of 16 columns whose
-// order inside the group is column_of's (PERMUTED columns).
-template <class T, int TERMS, int ROWS, int COLS, bool PAIRS, bool VEC, int THREADS = kRoleThreads> struct Operand {
-    static constexpr int kWide = PAIRS ? 16 : 8;
-    static constexpr int kAcross = COLS / kWide;
-    static constexpr int kItems = ROWS * kAcross / THREADS;
+// Operand block of ROWS rows and COLS columns, fetched in quads (a warp's accesses are contiguous: 16 or 32 lanes a row), its columns
+// in order or in column_of's (PERMUTED).  Shared memory is written without bank conflicts either way.
+template <class T, int TERMS, int ROWS, int COLS, bool PERMUTED, bool VEC, int THREADS = kRoleThreads> struct Operand {
+    static constexpr int kAcross = COLS / 4, kRows = THREADS / kAcross;   // quads a row, rows a pass
+    static constexpr int kItems = ROWS / kRows;
     static constexpr uint32_t kTermBytes = ROWS * COLS * 2;
     static constexpr uint32_t kBytes = TERMS * kTermBytes;
-    static_assert(ROWS * kAcross % THREADS == 0, "the threads share the items");
-    Piece<T> p[kItems][PAIRS ? 2 : 1];
+    static_assert(THREADS % kAcross == 0 && ROWS % kRows == 0 && kRows % 8 == 0, "whole passes, and a thread's rows at one place of the swizzle");
+    Quad<T> q[kItems];
 
-    // rows [row0, row_end) and columns [col0, col_end) of `from` are there, the rest is zero
-    // (t: this thread among the loaders)
+    // rows [row0, row_end) and columns [col0, col_end) of `from` are there, the rest is zero; t: this thread
     __device__ __forceinline__ void load(int t, const T* from, int64_t ld, int64_t row0, int64_t row_end, int col0, int col_end) {
-        const int row = t / kAcross, col = col0 + t % kAcross * kWide;
+        const int row = t / kAcross, col = col0 + t % kAcross * 4;
         const int rows = (int)min(row_end - row0, (int64_t)ROWS);
         const T* at = from + (row0 + row) * ld + col;
-        const int64_t step = ld * (THREADS / kAcross);
+        const int64_t step = ld * kRows;
 #pragma unroll
-        for (int i = 0; i < kItems; ++i, at += step) {
-            const int left = row + i * (THREADS / kAcross) < rows ? col_end - col : 0;
-            load_piece<VEC>(p[i][0], at, left);
-            if constexpr (PAIRS) load_piece<VEC>(p[i][1], at + 8, left - 8);
-        }
+        for (int i = 0; i < kItems; ++i, at += step) load_quad<VEC>(q[i], at, row + i * kRows < rows ? col_end - col : 0);
     }
     // PERMUTE_ROWS: the block's rows become the tile's columns
     template <bool PERMUTE_ROWS = false>
-    __device__ __forceinline__ void store(int thread, unsigned char* image) const {
+    __device__ __forceinline__ void store(int t, unsigned char* image) const {
+        static_assert(!PERMUTE_ROWS || kRows % 16 == 0, "a thread's rows at one place of their groups of 16");
+        const int across = t % kAcross, row = PERMUTE_ROWS ? column_of(t / kAcross) : t / kAcross;
+        unsigned char* const panel = image + (across >> 4) * (ROWS * 128);
+        const uint32_t at = PERMUTED ? image_offset(row, (across >> 1) & 6) + (across & 3) * 4
+                                     : image_offset(row, (across >> 1) & 7) + (across & 1) * 8;
+        const uint32_t behind = image_offset(row, ((across >> 1) & 6) + 1) + (across & 3) * 4;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            const int item = i * THREADS + thread;
-            int row = item / kAcross;
-            const int across = item % kAcross;
-            if constexpr (PERMUTE_ROWS) row = column_of(row);
-            uint32_t t[TERMS][4];
-            split<TERMS>(p[i][0], t);
-            if constexpr (!PAIRS) {
-                unsigned char* const at = image + (across >> 3) * (ROWS * 128) + image_offset(row, across & 7);
+            uint2 t2[TERMS];
+            split<TERMS>(q[i], t2);
 #pragma unroll
-                for (int k = 0; k < TERMS; ++k)
-                    *reinterpret_cast<uint4*>(at + k * kTermBytes) = make_uint4(t[k][0], t[k][1], t[k][2], t[k][3]);
-            } else {
-                uint32_t u[TERMS][4];
-                split<TERMS>(p[i][1], u);
-                unsigned char* const panel = image + (across >> 2) * (ROWS * 128);
-                const uint32_t even = image_offset(row, (across & 3) * 2), odd = image_offset(row, (across & 3) * 2 + 1);
-#pragma unroll
-                for (int k = 0; k < TERMS; ++k) {
-                    *reinterpret_cast<uint4*>(panel + k * kTermBytes + even) = make_uint4(t[k][0], t[k][2], u[k][0], u[k][2]);
-                    *reinterpret_cast<uint4*>(panel + k * kTermBytes + odd) = make_uint4(t[k][1], t[k][3], u[k][1], u[k][3]);
+            for (int k = 0; k < TERMS; ++k) {
+                unsigned char* const to = panel + i * (kRows * 128) + k * kTermBytes;
+                if constexpr (PERMUTED) {
+                    *reinterpret_cast<uint32_t*>(to + at) = t2[k].x;
+                    *reinterpret_cast<uint32_t*>(to + behind) = t2[k].y;
+                } else {
+                    *reinterpret_cast<uint2*>(to + at) = t2[k];
                 }
             }
         }
@@ -301,7 +261,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
     __shared__ uint64_t full[kMostStages], empty[kMostStages], tile_full[2], tile_empty[2], drain;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word, drain_word;
-    __shared__ float column_sums[P == kGradW ? 16 * NT : 1];
+    __shared__ float column_sums[P == kGradW ? OpB::kRows * NT : 1];   // (1024)
     __shared__ __align__(16) float bias[P == kForward || P == kSlope ? NT : 4];
     unsigned char* const smem = raw_smem + ((1024u - (umma::smem_addr(raw_smem) & 1023u)) & 1023u);
     volatile int* const abort_flag = &abort_word;
@@ -373,9 +333,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
             else if constexpr (P == kGradX) op_b.load(t, (const TB*)a.W, a.n_out, n0, a.n_in, chunk * kChunk, a.n_out);
             else op_b.load(t, (const TB*)a.W, a.n_out, chunk * kChunk, a.n_in, n0, a.n_out);
         };
-        float col_sum[P == kGradW ? 16 : 1];
-#pragma unroll
-        for (int i = 0; i < (P == kGradW ? 16 : 1); ++i) col_sum[i] = 0.f;
+        float col_sum[4] = {0.f, 0.f, 0.f, 0.f};   // kGradW: of this thread's four columns of gz, the same in every chunk
         if (units > 0) {
             load_a(0, 0);
             if (!a.resident) load_b(0, 0);
@@ -409,12 +367,9 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
                 if (!a.resident) {
                     op_b.template store<P == kGradX>(t, b_area + (size_t)stage * OpB::kBytes);
                     if constexpr (P == kGradW) {
-                        if (a.want_sums && m0 == 0) {
+                        if (a.want_sums && m0 == 0)
 #pragma unroll
-                            for (int i = 0; i < OpB::kItems; ++i)
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) col_sum[j] += element(op_b.p[i][j >> 3], j & 7);
-                        }
+                            for (int i = 0; i < OpB::kItems; ++i) op_b.q[i].add_to(col_sum);
                     }
                 }
                 if constexpr (L::kAsyncA) async_commit();
@@ -434,22 +389,13 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         while (ok && unreported > 0) report();
         if constexpr (P == kGradW) {
             if (a.want_sums && m0 == 0) {
-                // a thread's 16 columns are the same in every chunk; groups of threads in turn, 16 at a time
-                constexpr int kAcross = OpB::kAcross, kGroups = kRoleThreads / kAcross;
-                static_assert(kGroups % 16 == 0, "");
-                const int across = t % kAcross, group = t / kAcross;
-                for (int s = 0; s < kGroups / 16; ++s) {
-                    if (group / 16 == s)
+                const int across = t % OpB::kAcross, group = t / OpB::kAcross;
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            float* const at = &column_sums[(group % 16) * NT + across * 16 + j];
-                            *at = s == 0 ? col_sum[j] : *at + col_sum[j];
-                        }
-                    asm volatile("bar.sync 1, %0;" ::"n"(kRoleThreads) : "memory");
-                }
+                for (int j = 0; j < 4; ++j) column_sums[group * NT + across * 4 + j] = col_sum[j];
+                asm volatile("bar.sync 1, %0;" ::"n"(kRoleThreads) : "memory");
                 if (t < NT && n0 + t < a.n_out) {
                     float sum = 0.f;
-                    for (int r = 0; r < 16; ++r) sum += column_sums[r * NT + t];
+                    for (int r = 0; r < OpB::kRows; ++r) sum += column_sums[r * NT + t];
                     const int range = blockIdx.x / (a.n_tiles * a.m_tiles);
                     a.shares[(size_t)(range + 1) * ((size_t)a.n_in * a.n_out + a.n_out) - a.n_out + n0 + t] = sum;
                 }

@@ -28,7 +28,7 @@ template <Product P, class T, class G, int NT, int ACT, bool VEC>
 struct Launch {
     using L = LinTile<P, T, G, NT, VEC>;
     static constexpr auto kernel = linear_kernel<P, T, G, NT, ACT, VEC>;
-    static constexpr size_t kStatic = (P == kGradW ? 16 * NT : NT) * sizeof(float) + 512;
+    static constexpr size_t kStatic = (P == kGradW ? 1024 : NT) * sizeof(float) + 512;
     // Operand stages, and whether all of B's chunks stay in shared memory (with two stages at least).
     static int shape(LinArgs& a, int chunks, size_t& smem) {
         for (int resident = P == kGradW ? 0 : 1; resident >= 0; --resident)
