@@ -734,25 +734,29 @@ def e3j_conv_radial_vec_bwd(plan: Plan, x, edge_vec, h, W, senders, receivers, g
 
 
 # ----------------------------------------------------------------- the radial network's hidden layers
-_layer_types = {}   # torch.float32 -> E3J_F32, ...
+_layer_types = None   # torch.float32 -> E3J_F32, ...
 
 
 def _layer_call(x, tensors, stream):
     """The type code of a call on x [rows, n], and the context it runs in: None where x's device is the current one.  Every
     other tensor has to be on that device too."""
+    global _layer_types
     torch = _torch()
-    if not _layer_types:
-        _layer_types.update({torch.float32: E3J_F32, torch.bfloat16: E3J_BF16})
-    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+    if _layer_types is None:
+        _layer_types = {torch.float32: E3J_F32, torch.bfloat16: E3J_BF16}
+    here = _native is not None and stream is None and _native.same_device(x, *tensors) >= 0
+    if not here and (not isinstance(x, torch.Tensor) or not x.is_cuda):
         raise TypeError("x must be a CUDA tensor")
     code = _layer_types.get(x.dtype)
     if code is None:
         raise TypeError("x must be float32 or bfloat16")
     if x.dim() != 2:
         raise ValueError(f"x has shape {tuple(x.shape)}, expected [rows, columns]")
+    if here:
+        return code, None
     device = x.get_device()
     for t in tensors:
-        if isinstance(t, torch.Tensor) and t.get_device() != device:
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != device:   # (one on the host: refused with its name)
             raise ValueError("all tensors of a call must be on the same device")
     if stream is not None and getattr(stream, "device_index", device) != device:
         raise ValueError("the stream belongs to another device than the tensors")
@@ -782,7 +786,7 @@ def e3j_linear_fwd(x, W, b=None, residual=None, act: int = E3J_ACT_NONE, n_real=
 
 
 def e3j_linear_bwd_workspace_bytes(rows: int, n_in: int, n_out: int, act: int = E3J_ACT_NONE, dtype: int = E3J_F32) -> int:
-    return int(_load().e3j_linear_bwd_workspace_bytes(dtype, rows, n_in, n_out, act))
+    return _bytes("e3j_linear_bwd_workspace_bytes", dtype, rows, n_in, n_out, act)
 
 
 def e3j_linear_bwd(x, W, b, grad_y, act: int = E3J_ACT_NONE, n_real=None, grad_x=True, grad_W=True, grad_b=True,
@@ -796,7 +800,7 @@ def e3j_linear_bwd(x, W, b, grad_y, act: int = E3J_ACT_NONE, n_real=None, grad_x
     dtype, (rows, n_in), n_out = x.dtype, x.shape, W.shape[-1]
     grad_x, grad_W = _wanted(grad_x, (rows, n_in), dtype, x), _wanted(grad_W, (n_in, n_out), dtype, x)
     grad_b = _wanted(grad_b, (n_out,), dtype, x)
-    workspace = _workspace(int(_load().e3j_linear_bwd_workspace_bytes(code, rows, n_in, n_out, act)), x, workspace, stream)
+    workspace = _workspace(_bytes("e3j_linear_bwd_workspace_bytes", code, rows, n_in, n_out, act), x, workspace, stream)
     _run("e3j_linear_bwd", code, rows, n_in, n_out, _dev_ptr(x, dtype, None, "x"), _dev_ptr(W, dtype, (n_in, n_out), "W"),
          _dev_ptr(b, dtype, (n_out,), "b"), _dev_ptr(grad_y, dtype, (rows, n_out), "grad_y"), act,
          _dev_ptr(n_real, _torch_module.int32, (1,), "n_real"), _dev_ptr(grad_x, dtype, (rows, n_in), "grad_x"),
@@ -830,7 +834,7 @@ def e3j_layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, act: int = 
 
 
 def e3j_layer_norm_bwd_workspace_bytes(rows: int, n: int, dtype: int = E3J_F32) -> int:
-    return int(_load().e3j_layer_norm_bwd_workspace_bytes(dtype, rows, n))
+    return _bytes("e3j_layer_norm_bwd_workspace_bytes", dtype, rows, n)
 
 
 def e3j_layer_norm_bwd(x, weight, bias, grad_y, eps: float = 1e-5, act: int = E3J_ACT_NONE, n_real=None, grad_x=True,
@@ -844,7 +848,7 @@ def e3j_layer_norm_bwd(x, weight, bias, grad_y, eps: float = 1e-5, act: int = E3
     dtype, (rows, n) = x.dtype, x.shape
     grad_x, grad_weight = _wanted(grad_x, (rows, n), dtype, x), _wanted(grad_weight, (n,), dtype, x)
     grad_bias = _wanted(grad_bias, (n,), dtype, x)
-    workspace = _workspace(int(_load().e3j_layer_norm_bwd_workspace_bytes(code, rows, n)), x, workspace, stream)
+    workspace = _workspace(_bytes("e3j_layer_norm_bwd_workspace_bytes", code, rows, n), x, workspace, stream)
     _run_real("e3j_layer_norm_bwd", 7, float(eps), code, rows, n, _dev_ptr(x, dtype, None, "x"), _dev_ptr(weight, dtype, (n,), "weight"),
               _dev_ptr(bias, dtype, (n,), "bias"), _dev_ptr(grad_y, dtype, (rows, n), "grad_y"), act,
               _dev_ptr(n_real, _torch_module.int32, (1,), "n_real"), _dev_ptr(grad_x, dtype, (rows, n), "grad_x"),

@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -130,6 +131,20 @@ PyObject* call_real(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return invoke(args + 1, n - 1, kMostArgs, status, value) ? PyLong_FromLong(status) : nullptr;
 }
 
+// same_device(x, tensors...) -> x's device index where x and all that are not None (or truth values) are tensors on it, and it is the
+// current one; else -1: the binding looks into it.
+PyObject* same_device(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    int device = -1;
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        if (i > 0 && (args[i] == Py_None || PyBool_Check(args[i]))) continue;
+        if (!THPVariable_CheckExact(args[i])) return PyLong_FromLong(-1);
+        const at::Tensor& t = THPVariable_Unpack(args[i]);
+        if (!t.is_cuda() || (i > 0 && t.get_device() != device)) return PyLong_FromLong(-1);
+        device = (int)t.get_device();
+    }
+    return PyLong_FromLong(device >= 0 && c10::impl::VirtualGuardImpl(at::kCUDA).getDevice().index() == device ? device : -1);
+}
+
 // set_slow(dev_ptr, empty): what the two functions above fall back on
 PyObject* set_slow(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != 2) {
@@ -146,6 +161,7 @@ PyObject* set_slow(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef methods[] = {
     {"dev_ptr", (PyCFunction)(void (*)(void))dev_ptr, METH_FASTCALL, nullptr},
     {"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, nullptr},
+    {"same_device", (PyCFunction)(void (*)(void))same_device, METH_FASTCALL, nullptr},
     {"call_real", (PyCFunction)(void (*)(void))call_real, METH_FASTCALL, nullptr},
     {"call_size", (PyCFunction)(void (*)(void))call_size, METH_FASTCALL, nullptr},
     {"empty", (PyCFunction)(void (*)(void))empty, METH_FASTCALL, nullptr},

@@ -35,8 +35,11 @@
 namespace e3j {
 namespace layer {
 
-constexpr int kRoleThreads = 256;   // of the loaders, and of the readers
-constexpr int kLinThreads = 2 * kRoleThreads + 32;
+constexpr int kRoleThreads = 256;   // loaders
+// Reading warps: eight, or with bfloat16, whose loaders need few registers, sixteen (78 000 x 512 -> 512 with residual and GELU: RRR us
+// with eight).
+constexpr int read_warps(int size) { return size == 2 ? 16 : 8; }
+constexpr int lin_threads(int size) { return read_warps(size) * 32 + kRoleThreads + 32; }
 constexpr int kMostStages = 6;
 constexpr int kTileRows = 128;      // accumulator lanes
 constexpr int kChunk = 64;          // contraction elements a chunk
@@ -250,7 +253,7 @@ template <Product P, class T, class G, int NT, bool VEC> struct LinTile {
 };
 
 template <Product P, class T, class G, int NT, int ACT, bool VEC>
-__global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_constant__ LinArgs a) {
+__global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const __grid_constant__ LinArgs a) {
     using L = LinTile<P, T, G, NT, VEC>;
     using TA = typename L::Ty::A;
     using TB = typename L::Ty::B;
@@ -266,16 +269,17 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
     unsigned char* const smem = raw_smem + ((1024u - (umma::smem_addr(raw_smem) & 1023u)) & 1023u);
     volatile int* const abort_flag = &abort_word;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int kRoleWarps = kRoleThreads / 32;
+    constexpr int kLoaders = kRoleThreads / 32, kReaders = read_warps(sizeof(T)), kIssuer = kReaders + kLoaders;
+    constexpr int kWarpColumns = NT / (kReaders / 4);   // of a reading warp
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kMostStages; ++i) { fast::mbar_init(&full[i], kRoleWarps); fast::mbar_init(&empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { fast::mbar_init(&tile_full[i], 1); fast::mbar_init(&tile_empty[i], kRoleWarps); }
+        for (int i = 0; i < kMostStages; ++i) { fast::mbar_init(&full[i], kLoaders); fast::mbar_init(&empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { fast::mbar_init(&tile_full[i], 1); fast::mbar_init(&tile_empty[i], kReaders); }
         fast::mbar_init(&drain, 1);
         abort_word = drain_word = 0;
         fast::mbar_fence_init();
     }
-    if (warp == 2 * kRoleWarps) umma::tmem_alloc(&tmem_slot, L::kColumns);
+    if (warp == kIssuer) umma::tmem_alloc(&tmem_slot, L::kColumns);
     fast::grid_dependency_wait();
     fast::grid_dependency_trigger();
     const int nt = blockIdx.x % a.n_tiles;
@@ -314,9 +318,9 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
     };
     unsigned char* const b_area = smem + (size_t)a.stages * OpA::kBytes;
 
-    if (warp >= kRoleWarps && warp < 2 * kRoleWarps) {
+    if (warp >= kReaders && warp < kIssuer) {
         // ------------------------------------------------ loaders: memory -> terms -> stages
-        const int t = threadIdx.x - kRoleThreads;
+        const int t = threadIdx.x - kReaders * 32;
         OpA op_a;
         OpB op_b;
         auto with_a = [&](int unit, int chunk, auto&& f) {   // the block of A that a chunk takes
@@ -407,7 +411,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
             for (int64_t i = real * width + blockIdx.x * (int64_t)kRoleThreads + t; i < a.rows * width; i += (int64_t)gridDim.x * kRoleThreads)
                 out[i] = from_float<T>(0.f);
         }
-    } else if (warp == 2 * kRoleWarps) {
+    } else if (warp == kIssuer) {
         // ------------------------------------------------ tensor cores
         if (lane == 0) {
             const uint32_t a_addr = umma::smem_addr(smem), b_addr = umma::smem_addr(b_area);
@@ -456,17 +460,17 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         __syncwarp();
     } else {
         // ------------------------------------------------ readers: accumulators -> registers -> memory
-        const int half = warp >> 2, quarter = warp & 3;
-        float sums[P == kGradW ? NT / 2 : 1];
+        const int first = (warp >> 2) * kWarpColumns, quarter = warp & 3;   // 32 rows and kWarpColumns columns
+        float sums[P == kGradW ? kWarpColumns : 1];
 #pragma unroll
-        for (int i = 0; i < (P == kGradW ? NT / 2 : 1); ++i) sums[i] = 0.f;
+        for (int i = 0; i < (P == kGradW ? kWarpColumns : 1); ++i) sums[i] = 0.f;
         // What the results meet in memory, residual or grad_y, is fetched before the tile is waited for: kSlots groups of 16 columns
         // (as many as the registers hold), the others as these become free.
         constexpr bool kMeets = P == kForward || P == kSlope;
-        constexpr int kGroups = NT / 32, kSlots = !kMeets ? 1 : sizeof(T) == 4 ? 2 : kGroups;
+        constexpr int kGroups = kWarpColumns / 16, kSlots = !kMeets ? 1 : sizeof(T) == 4 ? 2 : kGroups;
         Quad<T> meets[kSlots][2][2];
         const int width = P == kGradX ? a.n_in : a.n_out;
-        const int f0 = n0 + half * (NT / 2) + 4 * (lane & 3);     // first of this lane's four features in the first group
+        const int f0 = n0 + first + 4 * (lane & 3);               // first of this lane's four features in the first group
         const T* const meet = (const T*)(P == kForward ? a.residual : a.grad_y);
         for (int unit = 0; unit < units; ++unit) {
             const int set = unit & 1;
@@ -485,7 +489,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
             umma::fence_after_sync();
 #pragma unroll
             for (int c = 0; c < kGroups; ++c) {
-                const int col = half * (NT / 2) + 16 * c;         // of the tile
+                const int col = first + 16 * c;                   // of the tile
                 const int f = f0 + 16 * c;
                 if (P != kGradW && n0 + col >= width) break;
 #pragma unroll
@@ -545,21 +549,21 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
             const int range = blockIdx.x / (a.n_tiles * a.m_tiles);
             float* const share = a.shares + (size_t)range * ((size_t)a.n_in * a.n_out + a.n_out);
 #pragma unroll
-            for (int c = 0; c < NT / 2; c += 16)
+            for (int c = 0; c < kGroups; ++c)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int row = m0 + quarter * 32 + h * 16 + ((i >> 1) & 1) * 8 + lane / 4;
-                        const int f = n0 + half * (NT / 2) + c + 4 * (lane & 3) + (i & 1) + ((i >> 2) << 1);
-                        if (row < a.n_in && f < a.n_out) share[(size_t)row * a.n_out + f] = sums[(c / 16 * 2 + h) * 8 + i];
+                        const int f = f0 + 16 * c + (i & 1) + ((i >> 2) << 1);
+                        if (row < a.n_in && f < a.n_out) share[(size_t)row * a.n_out + f] = sums[(c * 2 + h) * 8 + i];
                     }
         }
     }
     umma::fence_before_sync();
     __syncthreads();
     umma::fence_after_sync();
-    if (warp == 2 * kRoleWarps) umma::tmem_dealloc(tmem, L::kColumns);
+    if (warp == kIssuer) umma::tmem_dealloc(tmem, L::kColumns);
 }
 
 }  // namespace layer

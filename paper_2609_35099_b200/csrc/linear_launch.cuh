@@ -56,7 +56,7 @@ struct Launch {
             const int64_t per = std::max<int64_t>(sm_count() / a.n_tiles, 1);
             grid = a.n_tiles * std::min(per, row_tiles);
         }
-        return launch_dependent(kernel, dim3((unsigned)grid), dim3(kLinThreads), smem, st, a);
+        return launch_dependent(kernel, dim3((unsigned)grid), dim3(lin_threads(sizeof(T))), smem, st, a);
     }
 };
 
