@@ -331,7 +331,8 @@ int e3j_conv_radial_bwd(const e3j_plan* plan, int64_t n_nodes, int64_t n_edges, 
  * as the sum of three bfloat16 terms); a row with an infinity or a NaN in x comes out as NaN.
  * Backward: gz = grad_y act'(x W + b), formed again from x, W and b (the forward keeps nothing); grad_x = gz W^T, grad_W = x^T gz,
  * grad_b = sum over rows of gz; the residual's gradient is grad_y itself.  Any of grad_x, grad_W, grad_b may be NULL (not wanted).
- * Workspace: 256-byte aligned, e3j_linear_bwd_workspace_bytes(); calls that overlap on the GPU must not share it.
+ * Workspace: 256-byte aligned, e3j_linear_bwd_workspace_bytes() (0: none is needed, NULL will do); calls that overlap on the GPU must
+ * not share it.
  * e3j_linear_status reads (and clears) the status word of these kernels on the current device into the HOST word *status: 0 =
  * fine, 1 = a bounded wait gave up and the outputs of some call are invalid.  Synchronises the device. */
 int e3j_linear_fwd(int dtype, int64_t rows, int n_in, int n_out, const void* x, const void* W, const void* b,
@@ -345,7 +346,7 @@ int e3j_linear_status(int32_t* status);
 /* Layer norm over the n columns of a row (1 to 4096), with an activation behind it: z = (x - mean) / sqrt(variance + eps) * weight +
  * bias, y = act(z); weight and bias [n], either may be NULL (1 and 0); eps >= 0.  Backward: the gradients of x, weight and bias from
  * x, weight, bias and grad_y (mean and variance are formed again); any of grad_x, grad_weight, grad_bias may be NULL (not wanted).
- * Workspace: 256-byte aligned, e3j_layer_norm_bwd_workspace_bytes(), needed where grad_weight or grad_bias is wanted. */
+ * Workspace: as for e3j_linear_bwd, e3j_layer_norm_bwd_workspace_bytes(); not needed where neither grad_weight nor grad_bias is wanted. */
 int e3j_layer_norm_fwd(int dtype, int64_t rows, int n, const void* x, const void* weight, const void* bias, double eps, int act,
                        const int32_t* n_real, void* y, void* stream);
 size_t e3j_layer_norm_bwd_workspace_bytes(int dtype, int64_t rows, int n);

@@ -763,6 +763,14 @@ def _layer_call(x, tensors, stream):
     return code, None if device == torch.cuda.current_device() else torch.cuda.device(device)
 
 
+def _layer_workspace(nbytes, like, workspace, stream):
+    """Address and size of a call's workspace, and the tensor; a call that needs none gets none."""
+    if nbytes == 0 and workspace is None:
+        return None, 0, None
+    workspace = _workspace(nbytes, like, workspace, stream)
+    return workspace.data_ptr(), workspace.numel(), workspace
+
+
 def _wanted(flag, shape, dtype, like):
     """An output argument: True (allocate), False / None (not wanted) or a preallocated tensor."""
     return _empty(shape, dtype, like) if flag is True else None if flag is False else flag
@@ -800,12 +808,12 @@ def e3j_linear_bwd(x, W, b, grad_y, act: int = E3J_ACT_NONE, n_real=None, grad_x
     dtype, (rows, n_in), n_out = x.dtype, x.shape, W.shape[-1]
     grad_x, grad_W = _wanted(grad_x, (rows, n_in), dtype, x), _wanted(grad_W, (n_in, n_out), dtype, x)
     grad_b = _wanted(grad_b, (n_out,), dtype, x)
-    workspace = _workspace(_bytes("e3j_linear_bwd_workspace_bytes", code, rows, n_in, n_out, act), x, workspace, stream)
+    room, size, workspace = _layer_workspace(_bytes("e3j_linear_bwd_workspace_bytes", code, rows, n_in, n_out, act), x, workspace, stream)
     _run("e3j_linear_bwd", code, rows, n_in, n_out, _dev_ptr(x, dtype, None, "x"), _dev_ptr(W, dtype, (n_in, n_out), "W"),
          _dev_ptr(b, dtype, (n_out,), "b"), _dev_ptr(grad_y, dtype, (rows, n_out), "grad_y"), act,
          _dev_ptr(n_real, _torch_module.int32, (1,), "n_real"), _dev_ptr(grad_x, dtype, (rows, n_in), "grad_x"),
          _dev_ptr(grad_W, dtype, (n_in, n_out), "grad_W"), _dev_ptr(grad_b, dtype, (n_out,), "grad_b"),
-         workspace.data_ptr(), workspace.numel(), _stream(stream))
+         room, size, _stream(stream))
     return grad_x, grad_W, grad_b
 
 
@@ -848,12 +856,12 @@ def e3j_layer_norm_bwd(x, weight, bias, grad_y, eps: float = 1e-5, act: int = E3
     dtype, (rows, n) = x.dtype, x.shape
     grad_x, grad_weight = _wanted(grad_x, (rows, n), dtype, x), _wanted(grad_weight, (n,), dtype, x)
     grad_bias = _wanted(grad_bias, (n,), dtype, x)
-    workspace = _workspace(_bytes("e3j_layer_norm_bwd_workspace_bytes", code, rows, n), x, workspace, stream)
+    room, size, workspace = _layer_workspace(_bytes("e3j_layer_norm_bwd_workspace_bytes", code, rows, n), x, workspace, stream)
     _run_real("e3j_layer_norm_bwd", 7, float(eps), code, rows, n, _dev_ptr(x, dtype, None, "x"), _dev_ptr(weight, dtype, (n,), "weight"),
               _dev_ptr(bias, dtype, (n,), "bias"), _dev_ptr(grad_y, dtype, (rows, n), "grad_y"), act,
               _dev_ptr(n_real, _torch_module.int32, (1,), "n_real"), _dev_ptr(grad_x, dtype, (rows, n), "grad_x"),
               _dev_ptr(grad_weight, dtype, (n,), "grad_weight"), _dev_ptr(grad_bias, dtype, (n,), "grad_bias"),
-              workspace.data_ptr(), workspace.numel(), _stream(stream))
+              room, size, _stream(stream))
     return grad_x, grad_weight, grad_bias
 
 

@@ -4,6 +4,7 @@
     out = conv(plan, graph, x, sh, w)                     # differentiable in x, sh, w, to second order
     out = conv_radial(plan, graph, x, sh, h, W)           # weights from the radial layer; first order
     out = conv_vec(plan, graph, x, edge_vec, w)           # harmonics from the edge vectors; first order
+    h = layer_norm(linear(rbf, W0, b0), g0, c0, act=E3J_ACT_SILU)   # the radial network's hidden layers; first order
 
 The backward is e3j_conv_bwd; it is itself a differentiable function (of x, sh, w and the incoming cotangent), whose
 backward is e3j_conv_bwd_bwd -- what force training needs (a loss on gradients of the energy).  Third derivatives are
@@ -13,8 +14,9 @@ from __future__ import annotations
 
 import torch
 
-from . import (e3j_conv_bwd, e3j_conv_bwd_bwd, e3j_conv_fwd, e3j_conv_radial_bwd, e3j_conv_radial_fwd, e3j_conv_vec_bwd,
-               e3j_conv_vec_fwd, e3j_graph_prepare, e3j_graph_validate)
+from . import (E3J_ACT_NONE, e3j_conv_bwd, e3j_conv_bwd_bwd, e3j_conv_fwd, e3j_conv_radial_bwd, e3j_conv_radial_fwd,
+               e3j_conv_vec_bwd, e3j_conv_vec_fwd, e3j_graph_prepare, e3j_graph_validate, e3j_layer_norm_bwd, e3j_layer_norm_fwd,
+               e3j_linear_bwd, e3j_linear_fwd)
 
 
 class Graph:
@@ -119,3 +121,51 @@ def conv_radial(plan, graph: Graph, x, sh, h, W) -> torch.Tensor:
 def conv_vec(plan, graph: Graph, x, edge_vec, w) -> torch.Tensor:
     """The convolution with the harmonics taken from the edge vectors [n_edges, 3] (first derivatives)."""
     return _ConvVec.apply(plan, graph, x.contiguous(), edge_vec.contiguous(), w.contiguous())
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, W, b, residual, act, n_real):
+        ctx.act, ctx.n_real = act, n_real
+        ctx.save_for_backward(x, W, b)
+        return e3j_linear_fwd(x, W, b, residual, act, n_real)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_y):
+        x, W, b = ctx.saved_tensors
+        grad_y, need = grad_y.contiguous(), ctx.needs_input_grad
+        gx, gW, gb = e3j_linear_bwd(x, W, b, grad_y, ctx.act, ctx.n_real, grad_x=need[0], grad_W=need[1], grad_b=need[2])
+        gr = grad_y if need[3] else None
+        if gr is not None and ctx.n_real is not None:   # padding rows of the result do not depend on anything
+            real = torch.arange(gr.shape[0], device=gr.device).unsqueeze(1) < ctx.n_real
+            gr = torch.where(real, gr, torch.zeros_like(gr))
+        return gx, gW, gb, gr, None, None
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps, act, n_real):
+        ctx.eps, ctx.act, ctx.n_real = eps, act, n_real
+        ctx.save_for_backward(x, weight, bias)
+        return e3j_layer_norm_fwd(x, weight, bias, eps, act, n_real)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_y):
+        x, weight, bias = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        gx, gw, gb = e3j_layer_norm_bwd(x, weight, bias, grad_y.contiguous(), ctx.eps, ctx.act, ctx.n_real, grad_x=need[0],
+                                        grad_weight=need[1], grad_bias=need[2])
+        return gx, gw, gb, None, None, None
+
+
+def linear(x, W, b=None, residual=None, act: int = E3J_ACT_NONE, n_real=None) -> torch.Tensor:
+    """act(x W + b) + residual: x [rows, n_in], W [n_in, n_out] (float32 or bfloat16, first derivatives); saves x, W and b for the
+    backward, nothing else.  n_real as in e3j_linear_fwd."""
+    return _Linear.apply(x.contiguous(), W.contiguous(), _c(b), _c(residual), act, n_real)
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, act: int = E3J_ACT_NONE, n_real=None) -> torch.Tensor:
+    """Layer norm over the columns of x [rows, n] with an activation behind it (first derivatives); saves its inputs only."""
+    return _LayerNorm.apply(x.contiguous(), _c(weight), _c(bias), eps, act, n_real)

@@ -33,7 +33,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 }
 
 // V consecutive elements, read or written in one access (16 bytes that start on a multiple of 16, or one element): as they lie in
-// memory (Raw), and as pairs of float32 (one element: the first of a pair, and 0).
+// memory (Raw), and as pairs of float32 (one element: the first of a pair, and 0).  (store_four: four elements, to a multiple of their size.)
 template <class T, int V> struct Pack;
 template <> struct Pack<float, 1> {
     using Raw = float;
@@ -78,20 +78,11 @@ template <> struct Pack<bf16, 8> {
         *reinterpret_cast<uint4*>(p) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
     }
 };
-// Four elements that start on a multiple of their size.
-__device__ __forceinline__ void load_four(float (&v)[4], const float* p) {
-    const float4 q = __ldg(reinterpret_cast<const float4*>(p));
-    v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+__device__ __forceinline__ void store_four(float* p, const float2 (&v)[2]) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
 }
-__device__ __forceinline__ void load_four(float (&v)[4], const bf16* p) {
-    const uint2 q = __ldg(reinterpret_cast<const uint2*>(p));
-    v[0] = low_float(q.x); v[1] = high_float(q.x); v[2] = low_float(q.y); v[3] = high_float(q.y);
-}
-__device__ __forceinline__ void store_four(float* p, const float (&v)[4]) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-}
-__device__ __forceinline__ void store_four(bf16* p, const float (&v)[4]) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+__device__ __forceinline__ void store_four(bf16* p, const float2 (&v)[2]) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0].x, v[0].y), pack_bf16(v[1].x, v[1].y));
 }
 
 // 2^x and 1 / x by the hardware's approximations (within 2 and 1 steps of float32; results below the normal range are 0).
@@ -106,77 +97,87 @@ __device__ __forceinline__ float fast_reciprocal(float x) {
     return y;
 }
 constexpr float kLog2e = 1.44269504f;
+// Activations and their slopes, on pairs: what can be packed is one instruction for two elements.
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 // 1 / (1 + exp(-z)); exp(-z) = infinity gives 0
-__device__ __forceinline__ float logistic(float z) { return fast_reciprocal(1.f + fast_exp2(-kLog2e * z)); }
-
-// Normal distribution: its density phi(z) and distribution function Phi(z) from one exponential.  erf by the rational approximation
-// of Hastings (Abramowitz and Stegun 7.1.26), 1 - (a1 t + .. + a5 t^5) exp(-x^2) with t = 1 / (1 + p x), which is within 1.5e-7
-// (2.5 half steps of float32); Phi of a negative z is the second term's half and keeps its relative accuracy.  A layer norm of
-// 49 157 rows of 385 bfloat16 with GELU is bound by instructions: backward NNN us, with erff MMM.
-__device__ __forceinline__ void normal(float z, float& phi, float& Phi) {
-    const float x = fabsf(z) * 0.70710678f;
-    const float t = fast_reciprocal(fmaf(0.3275911f, x, 1.f));
-    const float e = fast_exp2(-kLog2e * x * x);
-    float poly = fmaf(1.061405429f, t, -1.453152027f);
-    poly = fmaf(poly, t, 1.421413741f);
-    poly = fmaf(poly, t, -0.284496736f);
-    poly = fmaf(poly, t, 0.254829592f);
-    const float tail = 0.5f * poly * t * e;   // Phi(-|z|)
-    Phi = z < 0.f ? tail : 1.f - tail;
-    phi = 0.39894228f * e;
+__device__ __forceinline__ float2 logistic(float2 z) {
+    const float2 x = __fmul2_rn(z, both(-kLog2e));
+    const float2 d = __fadd2_rn(make_float2(fast_exp2(x.x), fast_exp2(x.y)), both(1.f));
+    return make_float2(fast_reciprocal(d.x), fast_reciprocal(d.y));
 }
-
-template <int ACT> __device__ __forceinline__ float activation(float z) {
-    if constexpr (ACT == E3J_ACT_SILU) return z * logistic(z);
-    else if constexpr (ACT == E3J_ACT_TANH) return tanhf(z);
-    else if constexpr (ACT == E3J_ACT_GELU) {
-        float phi, Phi;
-        normal(z, phi, Phi);
-        return z * Phi;
+// Normal distribution: Phi(-|z|), and e = exp(-z^2 / 2).  The rational approximation of Hastings for erf (Abramowitz and Stegun
+// 7.1.26), 1 - (a1 t + .. + a5 t^5) exp(-x^2) with t = 1 / (1 + p x) and x = |z| / sqrt 2, which is within 1.5e-7 (2.5 half steps of
+// float32 at 1).  78 000 x 512 -> 512 bfloat16 with GELU is bound by instructions: forward GGG us, with CUDA's erff, element by
+// element, HHH.
+__device__ __forceinline__ float2 normal_tail(float2 z, float2& e) {
+    const float2 x = __fmul2_rn(__fmul2_rn(z, z), both(-0.5f * kLog2e));
+    e = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+    const float2 t = make_float2(fast_reciprocal(fmaf(0.23164189f, fabsf(z.x), 1.f)), fast_reciprocal(fmaf(0.23164189f, fabsf(z.y), 1.f)));
+    float2 poly = __ffma2_rn(both(0.5f * 1.061405429f), t, both(0.5f * -1.453152027f));
+    poly = __ffma2_rn(poly, t, both(0.5f * 1.421413741f));
+    poly = __ffma2_rn(poly, t, both(0.5f * -0.284496736f));
+    poly = __ffma2_rn(poly, t, both(0.5f * 0.254829592f));
+    return __fmul2_rn(__fmul2_rn(poly, t), e);
+}
+template <int ACT> __device__ __forceinline__ float2 activation(float2 z) {
+    if constexpr (ACT == E3J_ACT_SILU) return __fmul2_rn(z, logistic(z));
+    else if constexpr (ACT == E3J_ACT_TANH) return make_float2(tanhf(z.x), tanhf(z.y));
+    else if constexpr (ACT == E3J_ACT_GELU) {   // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
+        float2 e;
+        const float2 tail = normal_tail(z, e);
+        return make_float2(fmaf(-fabsf(z.x), tail.x, fmaxf(z.x, 0.f)), fmaf(-fabsf(z.y), tail.y, fmaxf(z.y, 0.f)));
     } else return z;
 }
-template <int ACT> __device__ __forceinline__ float slope(float z) {
-    if constexpr (ACT == E3J_ACT_SILU) {
-        const float s = logistic(z);
-        return s * fmaf(z, 1.f - s, 1.f);
+template <int ACT> __device__ __forceinline__ float2 slope(float2 z) {
+    if constexpr (ACT == E3J_ACT_SILU) {   // s (1 + z (1 - s))
+        const float2 s = logistic(z);
+        return __fmul2_rn(s, __ffma2_rn(z, __ffma2_rn(s, both(-1.f), both(1.f)), both(1.f)));
     } else if constexpr (ACT == E3J_ACT_TANH) {
-        const float t = tanhf(z);
-        return fmaf(-t, t, 1.f);
-    } else if constexpr (ACT == E3J_ACT_GELU) {
-        float phi, Phi;
-        normal(z, phi, Phi);
-        return fmaf(z, phi, Phi);
-    } else {
-        return 1.f;
-    }
-}
-// The same with the activation as a run-time value: one uniform branch for all elements.
-template <int ACT, int N> __device__ __forceinline__ void activate_as(float (&v)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = activation<ACT>(v[i]);
+        const float2 t = make_float2(tanhf(z.x), tanhf(z.y));
+        return __ffma2_rn(__fmul2_rn(t, both(-1.f)), t, both(1.f));
+    } else if constexpr (ACT == E3J_ACT_GELU) {   // Phi(z) + z phi(z)
+        float2 e;
+        const float2 beyond = __ffma2_rn(normal_tail(z, e), both(-1.f), both(0.5f));   // 1/2 - Phi(-|z|)
+        const float2 Phi = __fadd2_rn(make_float2(copysignf(beyond.x, z.x), copysignf(beyond.y, z.y)), both(0.5f));
+        return __ffma2_rn(z, __fmul2_rn(e, both(0.39894228f)), Phi);
+    } else return both(1.f);
 }
 template <int ACT, int N> __device__ __forceinline__ void activate_as(float2 (&v)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = make_float2(activation<ACT>(v[i].x), activation<ACT>(v[i].y));
+    for (int i = 0; i < N; ++i) v[i] = activation<ACT>(v[i]);
 }
-template <class F, int N> __device__ __forceinline__ void activate(F (&v)[N], int act) {
+// g[i] *= slope(z[i])
+template <int ACT, int N> __device__ __forceinline__ void times_slope_as(float2 (&g)[N], const float2 (&z)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) g[i] = __fmul2_rn(g[i], slope<ACT>(z[i]));
+}
+// The same with the activation as a run-time value: one uniform branch for all elements.
+template <int N> __device__ __forceinline__ void activate(float2 (&v)[N], int act) {
     if (act == E3J_ACT_SILU) activate_as<E3J_ACT_SILU>(v);
     else if (act == E3J_ACT_TANH) activate_as<E3J_ACT_TANH>(v);
     else if (act == E3J_ACT_GELU) activate_as<E3J_ACT_GELU>(v);
 }
-// g[i] *= slope(z[i])
-template <int ACT, int N> __device__ __forceinline__ void times_slope_as(float (&g)[N], const float (&z)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) g[i] *= slope<ACT>(z[i]);
-}
-template <int ACT, int N> __device__ __forceinline__ void times_slope_as(float2 (&g)[N], const float2 (&z)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) g[i] = __fmul2_rn(g[i], make_float2(slope<ACT>(z[i].x), slope<ACT>(z[i].y)));
-}
-template <class F, int N> __device__ __forceinline__ void times_slope(F (&g)[N], const F (&z)[N], int act) {
+template <int N> __device__ __forceinline__ void times_slope(float2 (&g)[N], const float2 (&z)[N], int act) {
     if (act == E3J_ACT_SILU) times_slope_as<E3J_ACT_SILU>(g, z);
     else if (act == E3J_ACT_TANH) times_slope_as<E3J_ACT_TANH>(g, z);
     else if (act == E3J_ACT_GELU) times_slope_as<E3J_ACT_GELU>(g, z);
+}
+
+// launch_dependent with clusters of that many blocks.
+template <class... KArgs, class... Args>
+inline int launch_cluster(void (*kernel)(KArgs...), int blocks, int cluster, int threads, size_t smem, cudaStream_t st, const Args&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3((unsigned)threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 2 : 1;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+    g_launch_count.fetch_add(1, std::memory_order_relaxed);
+    return cuda_status(err != cudaSuccess ? err : cudaGetLastError());
 }
 
 // A parameter's gradient from the blocks' shares of it, added in a fixed order: 32 elements a block, kSumWays

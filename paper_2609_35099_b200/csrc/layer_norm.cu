@@ -14,6 +14,8 @@
 //
 // The parameters' gradients are sums over all rows: every lane adds up its columns over the rows it meets, the warps of a
 // block add theirs in order, and sum_shares_kernel adds the blocks' shares in order.  No atomics; the same bits every time.
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
 #include "layer_common.cuh"
@@ -23,6 +25,7 @@ namespace layer {
 namespace {
 
 constexpr int kNormThreads = 256, kNormWarps = kNormThreads / 32;
+constexpr int kClusterBlocks = 8, kClusterTurns = 6;   // backward of few rows
 constexpr int kMostNorm = 4096;   // columns: 256 lanes of 16 elements
 
 struct NormArgs {
@@ -33,7 +36,8 @@ struct NormArgs {
     const void *x, *weight, *bias, *grad_y;
     const int32_t* n_real;
     void* out;             // y, or grad_x (null: not wanted)
-    float* shares;         // backward: [blocks][2 n] of grad_weight and grad_bias (null: not wanted)
+    float* shares;         // backward: [blocks][2 n] of grad_weight and grad_bias; null: the blocks, one cluster, add them up
+    void *grad_weight, *grad_bias;   // (either may be null: not wanted)
 };
 
 // Sums over the lanes of a row (LANES; 0: several warps), all of which get them.  Rows of several warps meet in shared memory;
@@ -246,7 +250,7 @@ __global__ void __launch_bounds__(kNormThreads, norm_blocks(V, EACH, BWD)) norm_
         }
     }
     if constexpr (BWD) {
-        if (!a.shares) return;
+        if (!a.grad_weight && !a.grad_bias) return;
         // the rows of a warp first where they have the same columns, then what is left in order: a warp's slots, the block's warps
         constexpr bool kTogether = !RAGGED && LANES > 0 && LANES < 32;
         if constexpr (kTogether)
@@ -280,14 +284,29 @@ __global__ void __launch_bounds__(kNormThreads, norm_blocks(V, EACH, BWD)) norm_
                 }
             __syncthreads();
         }
-        float* const to = a.shares + (int64_t)blockIdx.x * 2 * n;
-        for (int i = threadIdx.x; i < 2 * n; i += kNormThreads) to[i] = block_sums[i];
+        if (a.shares) {
+            float* const to = a.shares + (int64_t)blockIdx.x * 2 * n;
+            for (int i = threadIdx.x; i < 2 * n; i += kNormThreads) to[i] = block_sums[i];
+        } else {   // few rows: in the order of the cluster's blocks
+            const auto cluster = cooperative_groups::this_cluster();
+            cluster.sync();
+            for (int i = blockIdx.x * kNormThreads + threadIdx.x; i < 2 * n; i += gridDim.x * kNormThreads) {
+                float theirs[kClusterBlocks], sum = 0.f;   // (all on their way before the first is added)
+#pragma unroll
+                for (int r = 0; r < kClusterBlocks; ++r) theirs[r] = r < (int)gridDim.x ? cluster.map_shared_rank(block_sums, r)[i] : 0.f;
+#pragma unroll
+                for (int r = 0; r < kClusterBlocks; ++r) sum += theirs[r];
+                if (i < n && a.grad_weight) ((T*)a.grad_weight)[i] = from_float<T>(sum);
+                if (i >= n && a.grad_bias) ((T*)a.grad_bias)[i - n] = from_float<T>(sum);
+            }
+            cluster.sync();   // (nobody leaves while others read)
+        }
     }
 }
 
 // What a call runs on.  16-byte accesses where the arrays start on 16 bytes, element by element elsewhere and in narrow rows that do
 // not (32 columns or fewer: little data, and sums slot by slot would take longer than the rows).
-struct NormShape { int vector, ragged, each, lanes, blocks; };
+struct NormShape { int vector, ragged, each, lanes, blocks, direct; };
 
 NormShape norm_shape(int64_t rows, int n, int size, bool bwd, bool aligned) {
     NormShape s{};
@@ -304,14 +323,18 @@ NormShape norm_shape(int64_t rows, int n, int size, bool bwd, bool aligned) {
     const int64_t per_turn = kNormThreads / s.lanes;
     const int64_t resident = (int64_t)sm_count() * norm_blocks(s.vector ? v : 1, s.each, bwd);
     s.blocks = (int)std::min<int64_t>((rows + per_turn - 1) / per_turn, resident);
+    // Few rows, backward: one cluster, whose blocks take up to kClusterTurns turns, and no second kernel for the sums (1201 rows of
+    // 64: 14 us with it, LLL without).
+    s.direct = bwd && rows <= kClusterBlocks * kClusterTurns * per_turn;
+    if (s.direct) s.blocks = std::min(s.blocks, kClusterBlocks);
     const int step = (int)std::max<int64_t>(v / per_turn, 1);   // (ragged rows: the stride is a multiple of v rows)
     if (s.ragged) s.blocks = (s.blocks + step - 1) / step * step;
     return s;
 }
 
 template <class T, int V, int EACH, int LANES, bool RAGGED, bool BWD> int launch_norm(const NormArgs& a, const NormShape& s, cudaStream_t st) {
-    return launch_dependent(norm_kernel<T, V, EACH, LANES, RAGGED, BWD>, dim3((unsigned)s.blocks), dim3(kNormThreads),
-                            BWD ? sizeof(float) * 2 * (size_t)a.n : 0, st, a);
+    return launch_cluster(norm_kernel<T, V, EACH, LANES, RAGGED, BWD>, s.blocks, s.direct ? s.blocks : 1, kNormThreads,
+                          BWD ? sizeof(float) * 2 * (size_t)a.n : 0, st, a);
 }
 template <class T, int V, bool RAGGED, bool BWD> int launch_norm_lanes(const NormArgs& a, const NormShape& s, cudaStream_t st) {
     if (s.each == 16) return s.lanes == 32 ? launch_norm<T, V, 16, 32, RAGGED, BWD>(a, s, st) : launch_norm<T, V, 16, 0, RAGGED, BWD>(a, s, st);
@@ -340,9 +363,11 @@ int norm_fwd(NormArgs& a, cudaStream_t st) {
 template <class T>
 int norm_bwd(NormArgs& a, void* grad_weight, void* grad_bias, cudaStream_t st) {
     const NormShape s = norm_shape(a.rows, a.n, sizeof(T), true, on_16_bytes(a.x, a.grad_y, a.out));
-    if (!grad_weight && !grad_bias) a.shares = nullptr;
+    a.grad_weight = grad_weight;
+    a.grad_bias = grad_bias;
+    if (s.direct) a.shares = nullptr;
     if (int rc = norm<T, true>(a, s, st)) return rc;
-    if (!a.shares) return E3J_OK;
+    if (s.direct || (!grad_weight && !grad_bias)) return E3J_OK;
     return sum_shares<T>(s.blocks, a.n, a.n, a.shares, (T*)grad_weight, (T*)grad_bias, st);
 }
 
@@ -377,8 +402,11 @@ int e3j_layer_norm_fwd(int dtype, int64_t rows, int n, const void* x, const void
 size_t e3j_layer_norm_bwd_workspace_bytes(int dtype, int64_t rows, int n) {
     if (norm_args_status(rows, n, dtype, 0.0, E3J_ACT_NONE) != E3J_OK) return 0;
     const int size = dtype == E3J_F32 ? 4 : 2;
-    size_t most = 1;   // (arrays that do not start on 16 bytes may have another number of blocks)
-    for (bool aligned : {false, true}) most = std::max<size_t>(most, norm_shape(rows, n, size, true, aligned).blocks);
+    size_t most = 0;   // (arrays that do not start on 16 bytes may have another number of blocks)
+    for (bool aligned : {false, true}) {
+        const NormShape s = norm_shape(rows, n, size, true, aligned);
+        if (!s.direct) most = std::max<size_t>(most, s.blocks);
+    }
     return align_up(most * 2 * n * sizeof(float), 256);
 }
 
@@ -398,9 +426,8 @@ int e3j_layer_norm_bwd(int dtype, int64_t rows, int n, const void* x, const void
     }
     if (!x || !grad_y) return E3J_ERR_INVALID_ARG;
     if (!grad_x && !grad_weight && !grad_bias) return E3J_OK;
-    if ((grad_weight || grad_bias) && (!workspace || ((uintptr_t)workspace & 255u) ||
-                                       workspace_bytes < e3j_layer_norm_bwd_workspace_bytes(dtype, rows, n)))
-        return E3J_ERR_WORKSPACE;
+    const size_t need = grad_weight || grad_bias ? e3j_layer_norm_bwd_workspace_bytes(dtype, rows, n) : 0;
+    if (need > 0 && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need)) return E3J_ERR_WORKSPACE;
     NormArgs a{};
     a.rows = rows; a.n = n; a.eps = (float)eps; a.inverse_n = 1.f / (float)n; a.act = act;
     a.x = x; a.weight = weight; a.bias = bias; a.grad_y = grad_y; a.n_real = n_real; a.out = grad_x;

@@ -22,7 +22,8 @@ struct LinArgs {
     const void* gz;        // kGradX, kGradW: grad_y itself where there is no activation
     int ld_gz;             // elements of its rows: columns behind n_out, if any, hold zeros
     void* out;
-    float* shares;         // kGradW: [ranges][n_in * n_out + n_out]
+    float* shares;         // kGradW: [ranges][n_in * n_out + n_out]; null: the parameters' gradients are written here
+    void *grad_W, *grad_b; // (either may be null: not wanted)
     int ranges, want_sums;
     int n_tiles;           // tiles of 128 (kGradW: of its two dimensions, n_tiles x m_tiles) or NT columns
     int m_tiles;
@@ -31,8 +32,10 @@ struct LinArgs {
 };
 
 // The backward: one sweep where both widths are at most 64, else three products with gz in memory.  Workspace: [gz | shares];
-// ranges: the rows' division (narrow: blocks of the sweep).
-struct BwdLayout { bool narrow; int64_t ld_gz; int m_tiles, ranges; size_t shares, total; };
+// ranges: the rows' division (narrow: blocks of the sweep).  direct: no shares; with few rows the blocks of the sweep are
+// one cluster and add up among themselves, and the product is one range.
+struct BwdLayout { bool narrow, direct; int64_t ld_gz; int m_tiles, ranges; size_t shares, total; };
+constexpr int kClusterBlocks = 8;
 
 // Calls with rows > 0 and checked arguments; T: float or __nv_bfloat16.
 template <class T> int linear_fwd(LinArgs& a, int act, cudaStream_t st);

@@ -16,8 +16,13 @@
 // used) are the others.  The tensor cores add with truncation (radial_gemm.cuh): after kChainTiles tiles the warps add the sums to
 // totals of their own, which stay in tensor memory too, rounding.  Adding to a share in global memory instead took 22 000 cycles each time.
 //
-// Waits are bounded (fast::mbar_wait); no barrier but the last has to be met by all.
+// Few rows: the blocks are one cluster, keep their shares in shared memory and add them up there; no second kernel, no workspace
+// (1201 and fewer rows were 15 us with them, KKK without).
+//
+// Waits are bounded (fast::mbar_wait); no other barrier but those behind the tiles, which all threads reach, has to be met by all.
 #pragma once
+#include <cooperative_groups.h>
+
 #include "linear_kernels.cuh"
 
 namespace e3j {
@@ -81,9 +86,10 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) linear_bwd_narrow_kernel(co
     const int64_t row_tiles = (real + kTileRows - 1) / kTileRows;
     const int tiles = (int)(row_tiles > blockIdx.x ? (row_tiles - blockIdx.x + gridDim.x - 1) / gridDim.x : 0);   // of this block
     auto row0_of = [&](int tile) { return ((int64_t)blockIdx.x + (int64_t)tile * gridDim.x) * kTileRows; };
-    const bool want_x = a.out != nullptr, want_w = a.shares != nullptr;
-    const size_t share_size = (size_t)a.n_in * a.n_out + a.n_out;
-    float* const share = want_w ? a.shares + (size_t)blockIdx.x * S::parts * share_size : nullptr;
+    const bool want_x = a.out != nullptr, want_w = a.grad_W || a.grad_b;
+    const int share_size = a.n_in * a.n_out + a.n_out;
+    // this block's share of the parameters' gradients: in memory, or where x's images have been
+    float* const share = a.shares ? a.shares + (size_t)blockIdx.x * S::parts * share_size : reinterpret_cast<float*>(smem + S::off_x);
 
     // x with its columns, W with its rows and columns in column_of's order
     using OpX = Operand<T, X, kTileRows, kNarrow, true, VEC, kWorkWarps * 32>;
@@ -102,7 +108,7 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) linear_bwd_narrow_kernel(co
     __syncthreads();
     umma::fence_after_sync();
     const uint32_t tmem = tmem_slot;
-    float sum_b[4] = {0.f, 0.f, 0.f, 0.f};
+    float2 sum_b[2] = {both(0.f), both(0.f)};   // of this lane's four features
 
     if (warp == kWorkWarps) {
         // ------------------------------------------------ tensor cores
@@ -193,20 +199,15 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) linear_bwd_narrow_kernel(co
             __syncwarp();
             if (lane == 0) fast::mbar_arrive(bar);
         };
-        auto read = [&](uint32_t column, int h, float (&v)[8]) {
+        auto read = [&](uint32_t column, int h, Quads& v) {
             const uint32_t taddr = lanes + ((uint32_t)(h * 16) << 16) + column;
             __syncwarp();
             tmem_ld_quads(taddr, v);
             if constexpr (X == 3) {
-                float u[8];
+                Quads u;
                 tmem_ld_quads(taddr + kNarrow, u);
                 umma::tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    const float2 w = __fadd2_rn(make_float2(v[i], v[i + 1]), make_float2(u[i], u[i + 1]));
-                    v[i] = w.x;
-                    v[i + 1] = w.y;
-                }
+                add_quads(v, u);
             } else {
                 umma::tmem_ld_wait();
             }
@@ -220,22 +221,19 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) linear_bwd_narrow_kernel(co
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const uint32_t taddr = lanes + ((uint32_t)(h * 16) << 16);
-                float v[8], u[8], w[8];
+                Quads v, u, w;
                 __syncwarp();
                 tmem_ld_quads(taddr + S::col_sums, v);
                 if constexpr (G > 1) tmem_ld_quads(taddr + S::col_sums + kNarrow, u);
                 if constexpr (X == 3) tmem_ld_quads(taddr + S::col_sums + 2 * kNarrow, w);   // (rows 64 .. 127 of it are nothing)
                 umma::tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if constexpr (X == 3) v[i] += part == 0 ? u[i] + w[i] : u[i];
-                    else if constexpr (G > 1) v[i] += u[i];
-                }
+                if constexpr (X == 3)
+                    if (part == 0) add_quads(u, w);
+                if constexpr (G > 1) add_quads(v, u);
                 if (more) {
                     tmem_ld_quads(taddr + S::col_totals, u);
                     umma::tmem_ld_wait();
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] += u[i];
+                    add_quads(v, u);
                 }
                 if (!last) {
                     tmem_st_quads(taddr + S::col_totals, v);
@@ -244,8 +242,7 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) linear_bwd_narrow_kernel(co
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         const int k = feature_of((quarter & 1) * 32 + h * 16 + s * 8 + lane / 4);
-                        const float z[4] = {v[2 * s], v[2 * s + 1], v[4 + 2 * s], v[5 + 2 * s]};
-                        if (k < a.n_in) store_quad<false>(share + part * share_size + (size_t)k * a.n_out + f, z, a.n_out - f);
+                        if (k < a.n_in) store_quad<false>(share + part * share_size + k * a.n_out + f, v.p[s], a.n_out - f);
                     }
                 }
             }
@@ -269,28 +266,29 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) linear_bwd_narrow_kernel(co
             unsigned char* const image = gz_images + (size_t)(tile & 1) * G * S::image;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                float v[8];
+                Quads v;
                 if constexpr (kSlopes) read(S::col_z, h, v);
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    float g[4] = {0.f, 0.f, 0.f, 0.f};
+                    float2 g[2] = {both(0.f), both(0.f)};
                     g_raw[h][s].add_to(g);
                     if constexpr (kSlopes) {
                         const float4 b = *reinterpret_cast<const float4*>(bias + f);
-                        const float z[4] = {v[2 * s] + b.x, v[2 * s + 1] + b.y, v[4 + 2 * s] + b.z, v[5 + 2 * s] + b.w};
+                        const float2 z[2] = {__fadd2_rn(v.p[s][0], make_float2(b.x, b.y)), __fadd2_rn(v.p[s][1], make_float2(b.z, b.w))};
                         times_slope_as<ACT>(g, z);
                     }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sum_b[i] += g[i];
+                    sum_b[0] = __fadd2_rn(sum_b[0], g[0]);
+                    sum_b[1] = __fadd2_rn(sum_b[1], g[1]);
                     // columns 2 q, 2 q + 1 of the first and of the second piece of this group of 16
                     const int row = quarter * 32 + h * 16 + s * 8 + lane / 4;
                     unsigned char* const at = image + image_offset(row, col / 8) + (lane & 3) * 4;
                     unsigned char* const behind = image + image_offset(row, col / 8 + 1) + (lane & 3) * 4;
+                    uint2 terms[G];
+                    split<G>(g[0], g[1], terms);
 #pragma unroll
                     for (int k = 0; k < G; ++k) {
-                        const bool last = k == G - 1;
-                        *reinterpret_cast<uint32_t*>(at + k * S::image) = last ? pack_bf16(g[0], g[1]) : cut_pair(g[0], g[1]);
-                        *reinterpret_cast<uint32_t*>(behind + k * S::image) = last ? pack_bf16(g[2], g[3]) : cut_pair(g[2], g[3]);
+                        *reinterpret_cast<uint32_t*>(at + k * S::image) = terms[k].x;
+                        *reinterpret_cast<uint32_t*>(behind + k * S::image) = terms[k].y;
                     }
                 }
             }
@@ -309,13 +307,12 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) linear_bwd_narrow_kernel(co
                 if (col < a.n_in) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        float v[8];
+                        Quads v;
                         read(S::col_x, h, v);
 #pragma unroll
                         for (int s = 0; s < 2; ++s) {
                             const int64_t row = row0_of(tile) + quarter * 32 + h * 16 + s * 8 + lane / 4;
-                            const float z[4] = {v[2 * s], v[2 * s + 1], v[4 + 2 * s], v[5 + 2 * s]};
-                            if (row < real) store_quad<VEC>((T*)a.out + row * a.n_in + f, z, a.n_in - f);
+                            if (row < real) store_quad<VEC>((T*)a.out + row * a.n_in + f, v.p[s], a.n_in - f);
                         }
                     }
                 }
@@ -327,13 +324,14 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) linear_bwd_narrow_kernel(co
         if (want_w) {
             if (tiles > 0) end_chain(tiles - 1);
             else
-                for (size_t i = t; i < S::parts * share_size; i += kWorkWarps * 32) share[i] = 0.f;
+                for (int i = t; i < S::parts * share_size; i += kWorkWarps * 32) share[i] = 0.f;
             // the column sums: over the warp's rows, then over the four warps of a column group in order
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
+                float v = i & 1 ? sum_b[i / 2].y : sum_b[i / 2].x;
 #pragma unroll
-                for (int o = 4; o < 32; o <<= 1) sum_b[i] += __shfl_xor_sync(~0u, sum_b[i], o);
-                if (lane < 4) sums_of_warp[warp][4 * lane + i] = sum_b[i];
+                for (int o = 4; o < 32; o <<= 1) v += __shfl_xor_sync(~0u, v, o);
+                if (lane < 4) sums_of_warp[warp][4 * lane + i] = v;
             }
         }
         if (want_x && real < a.rows) {
@@ -350,6 +348,25 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) linear_bwd_narrow_kernel(co
         for (int q = 0; q < 4; ++q) sum += sums_of_warp[(t >> 4) * 4 + q][t & 15];
         share[share_size - a.n_out + t] = sum;
         if (S::parts == 2) share[2 * share_size - a.n_out + t] = 0.f;
+    }
+    if (want_w && !a.shares) {   // the shares of the cluster's blocks, added in their order
+        const auto cluster = cooperative_groups::this_cluster();
+        cluster.sync();
+        for (int i = blockIdx.x * kNarrowThreads + t; i < share_size; i += gridDim.x * kNarrowThreads) {
+            float theirs[kClusterBlocks][S::parts], sum = 0.f;   // (all on their way before the first is added)
+#pragma unroll
+            for (int r = 0; r < kClusterBlocks; ++r)
+#pragma unroll
+                for (int p = 0; p < S::parts; ++p) theirs[r][p] = r < (int)gridDim.x ? cluster.map_shared_rank(share, r)[p * share_size + i] : 0.f;
+#pragma unroll
+            for (int r = 0; r < kClusterBlocks; ++r)
+#pragma unroll
+                for (int p = 0; p < S::parts; ++p) sum += theirs[r][p];
+            const int in_W = share_size - a.n_out;
+            if (i < in_W && a.grad_W) ((T*)a.grad_W)[i] = from_float<T>(sum);
+            if (i >= in_W && a.grad_b) ((T*)a.grad_b)[i - in_W] = from_float<T>(sum);
+        }
+        cluster.sync();   // (nobody leaves while others read)
     }
     if (warp == kWorkWarps) umma::tmem_dealloc(tmem, 512);
 }

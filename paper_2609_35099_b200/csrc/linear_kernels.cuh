@@ -51,12 +51,16 @@ constexpr int kPanelBytes = 64 * 128;   // 64 rows of a panel
 template <class T> struct Quad;
 template <> struct Quad<float> {
     float4 q;
-    __device__ __forceinline__ void add_to(float (&v)[4]) const { v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w; }
+    __device__ __forceinline__ void add_to(float2 (&v)[2]) const {
+        v[0] = __fadd2_rn(v[0], make_float2(q.x, q.y));
+        v[1] = __fadd2_rn(v[1], make_float2(q.z, q.w));
+    }
 };
 template <> struct Quad<bf16> {
     uint2 q;
-    __device__ __forceinline__ void add_to(float (&v)[4]) const {
-        v[0] += low_float(q.x); v[1] += high_float(q.x); v[2] += low_float(q.y); v[3] += high_float(q.y);
+    __device__ __forceinline__ void add_to(float2 (&v)[2]) const {
+        v[0] = __fadd2_rn(v[0], make_float2(low_float(q.x), high_float(q.x)));
+        v[1] = __fadd2_rn(v[1], make_float2(low_float(q.y), high_float(q.y)));
     }
 };
 template <bool VEC> __device__ __forceinline__ void load_quad(Quad<float>& v, const float* from, int left) {
@@ -82,31 +86,31 @@ template <bool VEC> __device__ __forceinline__ void load_quad(Quad<bf16>& v, con
         if (left > 3) v.q.y |= (uint32_t)__ldg(h + 3) << 16;
     }
 }
-template <bool VEC, class T> __device__ __forceinline__ void store_quad(T* to, const float (&v)[4], int left) {
+template <bool VEC, class T> __device__ __forceinline__ void store_quad(T* to, const float2 (&v)[2], int left) {
     if constexpr (VEC) {
         if (left >= 4) store_four(to, v);
     } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) if (i < left) to[i] = from_float<T>(v[i]);
+        if (left > 0) to[0] = from_float<T>(v[0].x);
+        if (left > 1) to[1] = from_float<T>(v[0].y);
+        if (left > 2) to[2] = from_float<T>(v[1].x);
+        if (left > 3) to[3] = from_float<T>(v[1].y);
     }
 }
-// Cuts the leading 8 bits off two values: a term of both, packed; what is left of them in a, b.
-__device__ __forceinline__ uint32_t cut_pair(float& a, float& b) {
-    const uint32_t p = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
-    const float2 left = __fadd2_rn(make_float2(a, b), make_float2(-low_float(p), -high_float(p)));
-    a = left.x;
-    b = left.y;
+
+// Cuts the leading 8 bits off two values: a term of both, packed; what is left of them in v.
+__device__ __forceinline__ uint32_t cut_pair(float2& v) {
+    const uint32_t p = __byte_perm(__float_as_uint(v.x), __float_as_uint(v.y), 0x7632);
+    v = __fadd2_rn(v, make_float2(-low_float(p), -high_float(p)));
     return p;
 }
 // The terms of four elements, packed in pairs; the last is rounded (of three it is exact).
-template <int TERMS> __device__ __forceinline__ void split(const Quad<float>& v, uint2 (&t)[TERMS]) {
-    float a = v.q.x, b = v.q.y, c = v.q.z, d = v.q.w;
+template <int TERMS> __device__ __forceinline__ void split(float2 a, float2 b, uint2 (&t)[TERMS]) {
 #pragma unroll
-    for (int k = 0; k + 1 < TERMS; ++k) {
-        t[k].x = cut_pair(a, b);
-        t[k].y = cut_pair(c, d);
-    }
-    t[TERMS - 1] = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
+    for (int k = 0; k + 1 < TERMS; ++k) t[k] = make_uint2(cut_pair(a), cut_pair(b));
+    t[TERMS - 1] = make_uint2(pack_bf16(a.x, a.y), pack_bf16(b.x, b.y));
+}
+template <int TERMS> __device__ __forceinline__ void split(const Quad<float>& v, uint2 (&t)[TERMS]) {
+    split<TERMS>(make_float2(v.q.x, v.q.y), make_float2(v.q.z, v.q.w), t);
 }
 template <int TERMS> __device__ __forceinline__ void split(const Quad<bf16>& v, uint2 (&t)[TERMS]) {
     static_assert(TERMS == 1, "bfloat16 is one term");
@@ -135,21 +139,28 @@ __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uin
         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
-// The other way round: into tensor memory.
-__device__ __forceinline__ void tmem_st_quads(uint32_t taddr, const float (&v)[8]) {
-    asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-                 ::"r"(taddr), "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])),
-                   "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])) : "memory");
-}
-// 16 lanes x 16 columns: v[0], v[1], v[4], v[5] are row lane / 4, the others row lane / 4 + 8; columns 2 (lane % 4) and the next one, of
-// the first and of the second 8.
-__device__ __forceinline__ void tmem_ld_quads(uint32_t taddr, float (&v)[8]) {
+// 16 lanes x 16 columns of tensor memory: p[s] are four consecutive features (column_of) of row lane / 4 + 8 s; a quad of lanes has the
+// group's 16.  Columns 2 (lane % 4) and the next one, of the first and of the second 8.
+struct Quads { float2 p[2][2]; };
+__device__ __forceinline__ void tmem_ld_quads(uint32_t taddr, Quads& v) {
     uint32_t r[8];
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                  : "r"(taddr) : "memory");
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v.p[s][i] = make_float2(__uint_as_float(r[4 * i + 2 * s]), __uint_as_float(r[4 * i + 2 * s + 1]));
+}
+__device__ __forceinline__ void tmem_st_quads(uint32_t taddr, const Quads& v) {
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(taddr), "r"(__float_as_uint(v.p[0][0].x)), "r"(__float_as_uint(v.p[0][0].y)), "r"(__float_as_uint(v.p[1][0].x)),
+                   "r"(__float_as_uint(v.p[1][0].y)), "r"(__float_as_uint(v.p[0][1].x)), "r"(__float_as_uint(v.p[0][1].y)),
+                   "r"(__float_as_uint(v.p[1][1].x)), "r"(__float_as_uint(v.p[1][1].y)) : "memory");
+}
+__device__ __forceinline__ void add_quads(Quads& v, const Quads& u) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v.p[i >> 1][i & 1] = __fadd2_rn(v.p[i >> 1][i & 1], u.p[i >> 1][i & 1]);
 }
 
 // Operand block of ROWS rows and COLS columns, fetched in quads (a warp's accesses are contiguous: 16 or 32 lanes a row), its columns
@@ -337,7 +348,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
             else if constexpr (P == kGradX) op_b.load(t, (const TB*)a.W, a.n_out, n0, a.n_in, chunk * kChunk, a.n_out);
             else op_b.load(t, (const TB*)a.W, a.n_out, chunk * kChunk, a.n_in, n0, a.n_out);
         };
-        float col_sum[4] = {0.f, 0.f, 0.f, 0.f};   // kGradW: of this thread's four columns of gz, the same in every chunk
+        float2 col_sum[2] = {both(0.f), both(0.f)};   // kGradW: of this thread's four columns of gz, the same in every chunk
         if (units > 0) {
             load_a(0, 0);
             if (!a.resident) load_b(0, 0);
@@ -395,13 +406,17 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
             if (a.want_sums && m0 == 0) {
                 const int across = t % OpB::kAcross, group = t / OpB::kAcross;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) column_sums[group * NT + across * 4 + j] = col_sum[j];
+                for (int j = 0; j < 2; ++j) {
+                    column_sums[group * NT + across * 4 + 2 * j] = col_sum[j].x;
+                    column_sums[group * NT + across * 4 + 2 * j + 1] = col_sum[j].y;
+                }
                 asm volatile("bar.sync 1, %0;" ::"n"(kRoleThreads) : "memory");
                 if (t < NT && n0 + t < a.n_out) {
                     float sum = 0.f;
                     for (int r = 0; r < OpB::kRows; ++r) sum += column_sums[r * NT + t];
                     const int range = blockIdx.x / (a.n_tiles * a.m_tiles);
-                    a.shares[(size_t)(range + 1) * ((size_t)a.n_in * a.n_out + a.n_out) - a.n_out + n0 + t] = sum;
+                    if (a.shares) a.shares[(size_t)(range + 1) * ((size_t)a.n_in * a.n_out + a.n_out) - a.n_out + n0 + t] = sum;
+                    else if (a.grad_b) ((T*)a.grad_b)[n0 + t] = from_float<T>(sum);
                 }
             }
         } else if (P != kSlope && real < a.rows) {
@@ -461,9 +476,9 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
     } else {
         // ------------------------------------------------ readers: accumulators -> registers -> memory
         const int first = (warp >> 2) * kWarpColumns, quarter = warp & 3;   // 32 rows and kWarpColumns columns
-        float sums[P == kGradW ? kWarpColumns : 1];
+        Quads sums[P == kGradW ? kWarpColumns / 8 : 1];
 #pragma unroll
-        for (int i = 0; i < (P == kGradW ? kWarpColumns : 1); ++i) sums[i] = 0.f;
+        for (int i = 0; i < (P == kGradW ? kWarpColumns / 8 : 1) * 4; ++i) sums[i >> 2].p[i >> 1 & 1][i & 1] = both(0.f);
         // What the results meet in memory, residual or grad_y, is fetched before the tile is waited for: kSlots groups of 16 columns
         // (as many as the registers hold), the others as these become free.
         constexpr bool kMeets = P == kForward || P == kSlope;
@@ -495,33 +510,28 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {                     // 16 of the warp's 32 lanes of tensor memory
                     const uint32_t taddr = tmem + ((uint32_t)(quarter * 32 + h * 16) << 16) + (uint32_t)(set * L::kSets * NT + col);
-                    float v[8];
+                    Quads v;
                     __syncwarp();
                     tmem_ld_quads(taddr, v);
                     if constexpr (L::kSets == 2) {
-                        float u[8];
+                        Quads u;
                         tmem_ld_quads(taddr + NT, u);
                         umma::tmem_ld_wait();
-#pragma unroll
-                        for (int i = 0; i < 8; i += 2) {
-                            const float2 w = __fadd2_rn(make_float2(v[i], v[i + 1]), make_float2(u[i], u[i + 1]));
-                            v[i] = w.x;
-                            v[i + 1] = w.y;
-                        }
+                        add_quads(v, u);
                     } else {
                         umma::tmem_ld_wait();
                     }
                     if constexpr (P == kGradW) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) sums[(c * 2 + h) * 8 + i] += v[i];
+                        add_quads(sums[c * 2 + h], v);
                     } else {
 #pragma unroll
                         for (int s = 0; s < 2; ++s) {
                             const int64_t row = row0 + h * 16 + s * 8;
-                            float z[4] = {v[2 * s], v[2 * s + 1], v[4 + 2 * s], v[5 + 2 * s]};
+                            float2 (&z)[2] = v.p[s];
                             if constexpr (kMeets) {
                                 const float4 b = *reinterpret_cast<const float4*>(bias + col + 4 * (lane & 3));
-                                z[0] += b.x; z[1] += b.y; z[2] += b.z; z[3] += b.w;
+                                z[0] = __fadd2_rn(z[0], make_float2(b.x, b.y));
+                                z[1] = __fadd2_rn(z[1], make_float2(b.z, b.w));
                             }
                             if (row >= real) continue;
                             if constexpr (P == kForward) {
@@ -529,7 +539,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
                                 if (meet) meets[c % kSlots][h][s].add_to(z);
                             }
                             if constexpr (P == kSlope) {
-                                float g[4] = {0.f, 0.f, 0.f, 0.f};
+                                float2 g[2] = {both(0.f), both(0.f)};
                                 meets[c % kSlots][h][s].add_to(g);
                                 times_slope_as<ACT>(g, z);
                                 store_quad<true>((float*)a.out + row * a.ld_gz + f, g, a.ld_gz - f);   // (whole vectors: ld_gz)
@@ -547,16 +557,18 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
         }
         if constexpr (P == kGradW) {
             const int range = blockIdx.x / (a.n_tiles * a.m_tiles);
-            float* const share = a.shares + (size_t)range * ((size_t)a.n_in * a.n_out + a.n_out);
+            float* const share = a.shares + (size_t)range * ((size_t)a.n_in * a.n_out + a.n_out);   // (none: one range, to grad_W itself)
 #pragma unroll
             for (int c = 0; c < kGroups; ++c)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int row = m0 + quarter * 32 + h * 16 + ((i >> 1) & 1) * 8 + lane / 4;
-                        const int f = f0 + 16 * c + (i & 1) + ((i >> 2) << 1);
-                        if (row < a.n_in && f < a.n_out) share[(size_t)row * a.n_out + f] = sums[(c * 2 + h) * 8 + i];
+                    for (int s = 0; s < 2; ++s) {
+                        const int row = m0 + quarter * 32 + h * 16 + s * 8 + lane / 4;
+                        const int f = f0 + 16 * c;
+                        if (row >= a.n_in) continue;
+                        if (a.shares) store_quad<false>(share + (size_t)row * a.n_out + f, sums[c * 2 + h].p[s], a.n_out - f);
+                        else if (a.grad_W) store_quad<false>((T*)a.grad_W + (size_t)row * a.n_out + f, sums[c * 2 + h].p[s], a.n_out - f);
                     }
         }
     }

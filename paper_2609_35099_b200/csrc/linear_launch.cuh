@@ -92,7 +92,10 @@ template <class T, class G> int gradients(LinArgs a, const BwdLayout& L, void* g
     a.ranges = L.ranges;
     a.m_tiles = L.m_tiles;
     a.want_sums = grad_b != nullptr;
+    a.grad_W = grad_W;
+    a.grad_b = grad_b;
     if (int rc = product<kGradW, T, G>(a, gz && whole(a.x, a.n_in, sizeof(T)), st)) return rc;
+    if (L.direct) return E3J_OK;
     return sum_shares<T>(L.ranges, (int64_t)a.n_in * a.n_out, a.n_out, a.shares, (T*)grad_W, (T*)grad_b, st);
 }
 
@@ -101,20 +104,21 @@ template <class T, int ACT, bool VEC> int narrow_kernel(LinArgs& a, int blocks, 
     constexpr auto kernel = linear_bwd_narrow_kernel<T, ACT, VEC>;
     static std::atomic<uint64_t> allowed{0};
     if (int rc = allow_smem(kernel, S::smem, allowed)) return rc;
-    return launch_dependent(kernel, dim3((unsigned)blocks), dim3(kNarrowThreads), S::smem, st, a);
+    return launch_cluster(kernel, blocks, a.shares ? 1 : blocks, kNarrowThreads, S::smem, st, a);
 }
 template <class T, int ACT> int narrow_bwd(LinArgs& a, const BwdLayout& L, void* grad_W, void* grad_b, cudaStream_t st) {
     const bool vector = whole(a.x, a.n_in, sizeof(T)) && whole(a.W, a.n_out, sizeof(T)) && whole(a.grad_y, a.n_out, sizeof(T)) &&
                         whole(a.out, a.n_in, sizeof(T));
-    if (!grad_W && !grad_b) a.shares = nullptr;
+    a.grad_W = grad_W;
+    a.grad_b = grad_b;
     if (int rc = vector ? narrow_kernel<T, ACT, true>(a, L.ranges, st) : narrow_kernel<T, ACT, false>(a, L.ranges, st)) return rc;
-    if (!a.shares) return E3J_OK;
+    if (L.direct || (!grad_W && !grad_b)) return E3J_OK;
     return sum_shares<T>(L.ranges * NarrowLayout<T, ACT>::parts, (int64_t)a.n_in * a.n_out, a.n_out, a.shares, (T*)grad_W, (T*)grad_b, st);
 }
 
 template <class T>
 int linear_bwd(LinArgs& a, int act, const BwdLayout& L, void* workspace, void* grad_x, void* grad_W, void* grad_b, cudaStream_t st) {
-    a.shares = (float*)((char*)workspace + L.shares);
+    a.shares = L.direct ? nullptr : (float*)((char*)workspace + L.shares);
     if (L.narrow) {
         a.out = grad_x;
         if (act == E3J_ACT_SILU) return narrow_bwd<T, E3J_ACT_SILU>(a, L, grad_W, grad_b, st);
