@@ -52,6 +52,23 @@ template <> struct Pack<float, 4> {
     static __device__ __forceinline__ float2 pair(const Raw& q, int i) { return i ? make_float2(q.z, q.w) : make_float2(q.x, q.y); }
     static __device__ __forceinline__ Raw from(const float2 (&v)[2]) { return make_float4(v[0].x, v[0].y, v[1].x, v[1].y); }
     static __device__ __forceinline__ void store(float* p, const Raw& r) { *reinterpret_cast<float4*>(p) = r; }
+    // ones in the bits of the elements that f names; masking with them; storing those elements alone
+    template <class F> static __device__ __forceinline__ Raw ones(F f) {
+        const float one = __uint_as_float(~0u);
+        return make_float4(f(0) ? one : 0.f, f(1) ? one : 0.f, f(2) ? one : 0.f, f(3) ? one : 0.f);
+    }
+    static __device__ __forceinline__ float masked(float v, float m) { return __uint_as_float(__float_as_uint(v) & __float_as_uint(m)); }
+    template <int N, class M> static __device__ __forceinline__ void mask(Raw (&r)[N], const M& m) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            r[i] = make_float4(masked(r[i].x, m.r[i].x), masked(r[i].y, m.r[i].y), masked(r[i].z, m.r[i].z), masked(r[i].w, m.r[i].w));
+    }
+    static __device__ __forceinline__ void store_inside(float* p, const Raw& r, const Raw& m) {
+        if (__float_as_uint(m.x)) p[0] = r.x;
+        if (__float_as_uint(m.y)) p[1] = r.y;
+        if (__float_as_uint(m.z)) p[2] = r.z;
+        if (__float_as_uint(m.w)) p[3] = r.w;
+    }
 };
 template <> struct Pack<bf16, 1> {
     using Raw = uint16_t;
@@ -76,6 +93,27 @@ template <> struct Pack<bf16, 8> {
     }
     static __device__ __forceinline__ void store(bf16* p, const Raw& r) {
         *reinterpret_cast<uint4*>(p) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+    }
+    template <class F> static __device__ __forceinline__ Raw ones(F f) {
+        Raw m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m.w[i] = (f(2 * i) ? 0xffffu : 0u) | (f(2 * i + 1) ? 0xffff0000u : 0u);
+        return m;
+    }
+    template <int N, class M> static __device__ __forceinline__ void mask(Raw (&r)[N], const M& m) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) r[i].w[k] &= m.r[i].w[k];
+    }
+    static __device__ __forceinline__ void store_inside(bf16* p, const Raw& r, const Raw& m) {
+        uint16_t* const h = reinterpret_cast<uint16_t*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {   // (a pair at a time where both are inside)
+            if (m.w[i] == ~0u) *reinterpret_cast<uint32_t*>(h + 2 * i) = r.w[i];
+            if (m.w[i] == 0xffffu) h[2 * i] = (uint16_t)r.w[i];
+            if (m.w[i] == 0xffff0000u) h[2 * i + 1] = (uint16_t)(r.w[i] >> 16);
+        }
     }
 };
 __device__ __forceinline__ void store_four(float* p, const float2 (&v)[2]) {

@@ -67,10 +67,10 @@ template <int LANES> struct RowSum {
 };
 
 // Blocks an SM: as many as the registers allow (nearly) without spilling.
-__host__ __device__ constexpr int norm_blocks(int v, int each, bool bwd) {
+__host__ __device__ constexpr int norm_blocks(int v, int each, bool ragged, bool bwd) {
     return v == 1 ? (each == 8 && !bwd ? 2 : 1)
-         : each == 8 ? (!bwd ? 4 : v == 4 ? 2 : 3)
-         : v == 4 ? (bwd ? 1 : 2) : (bwd ? 2 : 3);
+         : each == 8 ? (!bwd ? (ragged ? 3 : 4) : v == 4 || ragged ? 2 : 3)
+         : v == 4 ? (bwd ? 1 : 2) : (bwd ? (ragged ? 1 : 2) : ragged ? 2 : 3);
 }
 
 // BWD: backward.  V elements an access, EACH a lane and row; LANES lanes a row (0: a.lanes of them, whole warps).
@@ -78,11 +78,11 @@ __host__ __device__ constexpr int norm_blocks(int v, int each, bool bwd) {
 // the left of it; the grid's stride is a multiple of V rows, so a slot's rows all have the same shift and its lanes keep
 // their columns.  Accesses that reach over an end of the row go element by element.
 template <class T, int V, int EACH, int LANES, bool RAGGED, bool BWD>
-__global__ void __launch_bounds__(kNormThreads, norm_blocks(V, EACH, BWD)) norm_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kNormThreads, norm_blocks(V, EACH, RAGGED, BWD)) norm_kernel(const NormArgs a) {
     constexpr int NV = EACH / V;
     using P = Pack<T, V>;
     constexpr int H = P::kPairs, E2 = NV * H;   // pairs of an access, of a lane
-    extern __shared__ float block_sums[];       // backward: [2][n]
+    extern __shared__ float block_sums[];       // backward: [warps or slots][2][n], the first row then the block's
     __shared__ float2 meet[2 * kNormWarps];
     const int n = a.n, lanes = LANES ? LANES : a.lanes;
     const int slots = kNormThreads / lanes, slot = threadIdx.x / lanes, lane = threadIdx.x % lanes;
@@ -127,6 +127,10 @@ __global__ void __launch_bounds__(kNormThreads, norm_blocks(V, EACH, BWD)) norm_
             for (int i = 0; i < NV; ++i) p.r[i] = P::none();
         }
     };
+    Part masks;   // RAGGED: ones in the bits of the columns inside the row
+    if constexpr (RAGGED)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) masks.r[i] = P::ones([&](int j) { return inside(col(i) + j); });
     // this lane's columns of the parameters; columns outside the row: 0
     Part w, b;
     {
@@ -156,29 +160,19 @@ __global__ void __launch_bounds__(kNormThreads, norm_blocks(V, EACH, BWD)) norm_
                 for (int i = 0; i < NV; ++i) {
                     T* const at = out + row * n + col(i);
                     if (whole(i)) P::store(at, P::none());
-                    else if (RAGGED && col(i) < n)
-#pragma unroll
-                        for (int j = 0; j < V; ++j)
-                            if (inside(col(i) + j)) at[j] = from_float<T>(0.f);
+                    else if constexpr (RAGGED) P::store_inside(at, P::none(), masks.r[i]);
                 }
             continue;
         }
         float2 v[E2], g[BWD ? E2 : 1];
+        if constexpr (RAGGED) {   // (without what an access took in from outside the row)
+            P::mask(next_x.r, masks);
+            if constexpr (BWD) P::mask(next_g.r, masks);
+        }
 #pragma unroll
         for (int k = 0; k < E2; ++k) {
             v[k] = P::pair(next_x.r[k / H], k % H);
             if constexpr (BWD) g[k] = P::pair(next_g.r[k / H], k % H);
-        }
-        if constexpr (RAGGED) {   // what an access took in from outside the row
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (!whole(i))
-#pragma unroll
-                    for (int j = 0; j < V; ++j)
-                        if (!inside(col(i) + j)) {
-                            (j & 1 ? v[i * H + j / 2].y : v[i * H + j / 2].x) = 0.f;
-                            if constexpr (BWD) (j & 1 ? g[i * H + j / 2].y : g[i * H + j / 2].x) = 0.f;
-                        }
         }
         fetch(next_x, x, row + stride);
         if constexpr (BWD) fetch(next_g, gy, row + stride);
@@ -189,20 +183,21 @@ __global__ void __launch_bounds__(kNormThreads, norm_blocks(V, EACH, BWD)) norm_
         float2 square = make_float2(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
+            // (outside the row v becomes -mean, which nothing but this sum sees: weight, bias and grad_y are 0 there)
             if (whole(i)) {
 #pragma unroll
                 for (int j = 0; j < H; ++j) {
-                    v[i * H + j] = V == 1 ? make_float2(v[i * H].x - mean, 0.f) : __fadd2_rn(v[i * H + j], make_float2(-mean, -mean));
+                    v[i * H + j] = V == 1 ? make_float2(v[i * H].x - mean, 0.f) : __fadd2_rn(v[i * H + j], both(-mean));
+                    square = __ffma2_rn(v[i * H + j], v[i * H + j], square);
                 }
             } else if (RAGGED) {   // (without, there is nothing but zeros here)
 #pragma unroll
                 for (int j = 0; j < H; ++j) {
-                    if (inside(col(i) + 2 * j)) v[i * H + j].x -= mean;
-                    if (inside(col(i) + 2 * j + 1)) v[i * H + j].y -= mean;
+                    v[i * H + j] = __fadd2_rn(v[i * H + j], both(-mean));
+                    if (inside(col(i) + 2 * j)) square.x = fmaf(v[i * H + j].x, v[i * H + j].x, square.x);
+                    if (inside(col(i) + 2 * j + 1)) square.y = fmaf(v[i * H + j].y, v[i * H + j].y, square.y);
                 }
             }
-#pragma unroll
-            for (int j = 0; j < H; ++j) square = __ffma2_rn(v[i * H + j], v[i * H + j], square);
         }
         const float variance = row_sum(square.x + square.y) * a.inverse_n;
         // (a padding row is zero throughout, also with eps = 0)
@@ -240,12 +235,9 @@ __global__ void __launch_bounds__(kNormThreads, norm_blocks(V, EACH, BWD)) norm_
                 float2 o[H];
 #pragma unroll
                 for (int j = 0; j < H; ++j) o[j] = z[i * H + j];
-                if (whole(i)) P::store(at + col(i), row < real ? P::from(o) : P::none());
-                else if (RAGGED && col(i) < n) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j)
-                        if (inside(col(i) + j)) at[col(i) + j] = from_float<T>(row < real ? (j & 1 ? o[j / 2].y : o[j / 2].x) : 0.f);
-                }
+                const typename P::Raw r = row < real ? P::from(o) : P::none();
+                if (whole(i)) P::store(at + col(i), r);
+                else if constexpr (RAGGED) P::store_inside(at + col(i), r, masks.r[i]);
             }
         }
     }
@@ -263,27 +255,35 @@ __global__ void __launch_bounds__(kNormThreads, norm_blocks(V, EACH, BWD)) norm_
                     sum_b[k].x += __shfl_xor_sync(~0u, sum_b[k].x, o);
                     sum_b[k].y += __shfl_xor_sync(~0u, sum_b[k].y, o);
                 }
-        for (int i = threadIdx.x; i < 2 * n; i += kNormThreads) block_sums[i] = 0.f;
-        __syncthreads();
-        const int turns = LANES ? kNormWarps : slots, turn = LANES ? (int)threadIdx.x >> 5 : slot;
-        const int per_warp = LANES > 0 && LANES < 32 && !kTogether ? 32 / lanes : 1;
-        for (int t = 0; t < turns; ++t) {
-            if (t == turn)
-                for (int s = 0; s < per_warp; ++s) {
-                    if (LANES == 0 || (int)(threadIdx.x & 31) / lanes == s)
-#pragma unroll
-                        for (int i = 0; i < NV; ++i)
-#pragma unroll
-                            for (int j = 0; j < V; ++j)
-                                if (inside(col(i) + j)) {
-                                    const float2 sw = sum_w[i * H + j / 2], sb = sum_b[i * H + j / 2];
-                                    block_sums[col(i) + j] += j & 1 ? sw.y : sw.x;
-                                    block_sums[n + col(i) + j] += j & 1 ? sb.y : sb.x;
-                                }
-                    __syncwarp();
-                }
-            __syncthreads();
+        // every warp (or slot of several warps) leaves its sums in a row of its own
+        const int rows_of_sums = LANES ? kNormWarps : slots;
+        float* const mine = block_sums + (LANES ? (int)threadIdx.x >> 5 : slot) * 2 * n;
+        if constexpr (RAGGED && LANES > 0 && LANES < 32) {   // (a warp's slots have other columns: one after another)
+            for (int i = threadIdx.x & 31; i < 2 * n; i += 32) mine[i] = 0.f;
+            __syncwarp();
         }
+        const int speakers = RAGGED && LANES > 0 && LANES < 32 ? 32 / lanes : 1;
+        for (int s = 0; s < speakers; ++s) {
+            if (LANES == 0 || (int)(threadIdx.x & 31) / lanes == s)
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        if (inside(col(i) + j)) {
+                            const float2 sw = sum_w[i * H + j / 2], sb = sum_b[i * H + j / 2];
+                            float *pw = mine + col(i) + j, *pb = pw + n;
+                            *pw = (speakers > 1 ? *pw : 0.f) + (j & 1 ? sw.y : sw.x);
+                            *pb = (speakers > 1 ? *pb : 0.f) + (j & 1 ? sb.y : sb.x);
+                        }
+            __syncwarp();
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * n; i += kNormThreads) {
+            float sum = block_sums[i];
+            for (int r = 1; r < rows_of_sums; ++r) sum += block_sums[r * 2 * n + i];
+            block_sums[i] = sum;
+        }
+        __syncthreads();
         if (a.shares) {
             float* const to = a.shares + (int64_t)blockIdx.x * 2 * n;
             for (int i = threadIdx.x; i < 2 * n; i += kNormThreads) to[i] = block_sums[i];
@@ -316,12 +316,12 @@ NormShape norm_shape(int64_t rows, int n, int size, bool bwd, bool aligned) {
     // Elements a lane: 8, or 16 in rows of more than 256 (fewer lanes to sum over) unless the backward's registers would not
     // hold them, and whenever 8 are not enough.
     const int width = n + (s.ragged ? v - 1 : 0);
-    s.each = width > 8 * kNormThreads || (width > 256 && (!bwd || (size == 2 && s.vector))) ? 16 : 8;
+    s.each = width > 8 * kNormThreads || (width > 256 && (!bwd || (size == 2 && s.vector && !s.ragged))) ? 16 : 8;
     s.lanes = 1;
     while (s.lanes * s.each < width) s.lanes *= 2;
     if (s.each == 16) s.lanes = std::max(s.lanes, 32);
     const int64_t per_turn = kNormThreads / s.lanes;
-    const int64_t resident = (int64_t)sm_count() * norm_blocks(s.vector ? v : 1, s.each, bwd);
+    const int64_t resident = (int64_t)sm_count() * norm_blocks(s.vector ? v : 1, s.each, s.ragged, bwd);
     s.blocks = (int)std::min<int64_t>((rows + per_turn - 1) / per_turn, resident);
     // Few rows, backward: one cluster, whose blocks take up to kClusterTurns turns, and no second kernel for the sums (1201 rows of
     // 64: 14 us with it, LLL without).
@@ -334,7 +334,7 @@ NormShape norm_shape(int64_t rows, int n, int size, bool bwd, bool aligned) {
 
 template <class T, int V, int EACH, int LANES, bool RAGGED, bool BWD> int launch_norm(const NormArgs& a, const NormShape& s, cudaStream_t st) {
     return launch_cluster(norm_kernel<T, V, EACH, LANES, RAGGED, BWD>, s.blocks, s.direct ? s.blocks : 1, kNormThreads,
-                          BWD ? sizeof(float) * 2 * (size_t)a.n : 0, st, a);
+                          BWD ? sizeof(float) * 2 * (size_t)a.n * (LANES ? kNormWarps : kNormThreads / s.lanes) : 0, st, a);   // (32 KB at most)
 }
 template <class T, int V, bool RAGGED, bool BWD> int launch_norm_lanes(const NormArgs& a, const NormShape& s, cudaStream_t st) {
     if (s.each == 16) return s.lanes == 32 ? launch_norm<T, V, 16, 32, RAGGED, BWD>(a, s, st) : launch_norm<T, V, 16, 0, RAGGED, BWD>(a, s, st);

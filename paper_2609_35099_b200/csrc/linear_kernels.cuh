@@ -36,9 +36,8 @@ namespace e3j {
 namespace layer {
 
 constexpr int kRoleThreads = 256;   // loaders
-// Reading warps: eight, or with bfloat16, whose loaders need few registers, sixteen (78 000 x 512 -> 512 with residual and GELU: RRR us
-// with eight).
-constexpr int read_warps(int size) { return size == 2 ? 16 : 8; }
+// Reading warps: sixteen, but for float32, whose loaders need the registers, eight (60 000 x 256 -> 256 with residual, with sixteen: 122 us).
+constexpr int read_warps(int size) { return size == 4 ? 8 : 16; }
 constexpr int lin_threads(int size) { return read_warps(size) * 32 + kRoleThreads + 32; }
 constexpr int kMostStages = 6;
 constexpr int kTileRows = 128;      // accumulator lanes
@@ -68,6 +67,7 @@ template <bool VEC> __device__ __forceinline__ void load_quad(Quad<float>& v, co
     if constexpr (VEC) {
         if (left >= 4) v.q = __ldg(reinterpret_cast<const float4*>(from));
     } else {
+        // (four predicates, no branch: the loads of all quads go out together)
         if (left > 0) v.q.x = __ldg(from);
         if (left > 1) v.q.y = __ldg(from + 1);
         if (left > 2) v.q.z = __ldg(from + 2);
@@ -251,21 +251,22 @@ template <class T, class G> struct Types<kGradW, T, G> {
     static constexpr int a_terms = sizeof(T) == 4 ? 3 : 1, b_terms = sizeof(G) == 2 ? 1 : sizeof(T) == 4 ? 3 : 2;
 };
 
-template <Product P, class T, class G, int NT, bool VEC> struct LinTile {
+// VA: A's rows start on 16 bytes; VO: those of B, of the results and of what they meet do.
+template <Product P, class T, class G, int NT, bool VA, bool VO> struct LinTile {
     using Ty = Types<P, T, G>;
     static constexpr bool kRowSum = P == kGradW;    // contraction over rows: both operands MN-major
-    using OpA = Operand<typename Ty::A, Ty::a_terms, kRowSum ? kChunk : kTileRows, kRowSum ? kTileRows : kChunk, false, VEC>;
-    using OpB = Operand<typename Ty::B, Ty::b_terms, P == kGradX ? NT : kChunk, P == kGradX ? kChunk : NT, P != kGradX, VEC>;
+    using OpA = Operand<typename Ty::A, Ty::a_terms, kRowSum ? kChunk : kTileRows, kRowSum ? kTileRows : kChunk, false, VA>;
+    using OpB = Operand<typename Ty::B, Ty::b_terms, P == kGradX ? NT : kChunk, P == kGradX ? kChunk : NT, P != kGradX, VO>;
     static constexpr bool kA_mn = kRowSum, kB_mn = P != kGradX;
     static constexpr int kSets = Ty::a_terms == 3 ? 2 : 1;     // accumulators of a tile
     static constexpr int kColumns = 2 * kSets * NT;            // tensor memory: two tiles
-    static constexpr bool kAsyncA = VEC && sizeof(typename Ty::A) == 2;   // A by cp.async
+    static constexpr bool kAsyncA = VA && sizeof(typename Ty::A) == 2;   // A by cp.async
     static size_t smem_bytes(int stages, int b_slots) { return 1024 + (size_t)stages * OpA::kBytes + (size_t)b_slots * OpB::kBytes; }
 };
 
-template <Product P, class T, class G, int NT, int ACT, bool VEC>
+template <Product P, class T, class G, int NT, int ACT, bool VA, bool VO>
 __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const __grid_constant__ LinArgs a) {
-    using L = LinTile<P, T, G, NT, VEC>;
+    using L = LinTile<P, T, G, NT, VA, VO>;
     using TA = typename L::Ty::A;
     using TB = typename L::Ty::B;
     using OpA = typename L::OpA;
@@ -298,10 +299,6 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
     if constexpr (P == kForward || P == kSlope)
         if (threadIdx.x < NT)
             bias[threadIdx.x] = a.b && n0 + (int)threadIdx.x < a.n_out ? to_float(((const T*)a.b)[n0 + threadIdx.x]) : 0.f;
-    umma::fence_before_sync();
-    __syncthreads();
-    umma::fence_after_sync();
-    const uint32_t tmem = tmem_slot;
     const int64_t real = real_rows(a.rows, a.n_real);
 
     // ---- what this block does: units (a tile, or for kGradW a group of chunks of one tile) of `chunks` chunks
@@ -328,6 +325,22 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
         else return chunks;
     };
     unsigned char* const b_area = smem + (size_t)a.stages * OpA::kBytes;
+    auto load_w = [&](OpB& op, int t, int chunk) {
+        if constexpr (P == kGradX) op.load(t, (const TB*)a.W, a.n_out, n0, a.n_in, chunk * kChunk, a.n_out);
+        else if constexpr (P != kGradW) op.load(t, (const TB*)a.W, a.n_out, chunk * kChunk, a.n_in, n0, a.n_out);
+    };
+    if (a.resident && units > 0) {   // all warps bring B in, a chunk for each 256 threads
+        for (int k = threadIdx.x / kRoleThreads; k < chunks && warp < kIssuer; k += kIssuer * 32 / kRoleThreads) {
+            OpB op;
+            load_w(op, threadIdx.x % kRoleThreads, k);
+            op.template store<P == kGradX>(threadIdx.x % kRoleThreads, b_area + (size_t)k * OpB::kBytes);
+        }
+        umma::fence_smem_to_async();
+    }
+    umma::fence_before_sync();
+    __syncthreads();
+    umma::fence_after_sync();
+    const uint32_t tmem = tmem_slot;
 
     if (warp >= kReaders && warp < kIssuer) {
         // ------------------------------------------------ loaders: memory -> terms -> stages
@@ -345,18 +358,12 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
         };
         auto load_b = [&](int unit, int chunk) {
             if constexpr (P == kGradW) op_b.load(t, (const TB*)a.gz, a.ld_gz, (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunk, real, n0, a.ld_gz);
-            else if constexpr (P == kGradX) op_b.load(t, (const TB*)a.W, a.n_out, n0, a.n_in, chunk * kChunk, a.n_out);
-            else op_b.load(t, (const TB*)a.W, a.n_out, chunk * kChunk, a.n_in, n0, a.n_out);
+            else load_w(op_b, t, chunk);
         };
         float2 col_sum[2] = {both(0.f), both(0.f)};   // kGradW: of this thread's four columns of gz, the same in every chunk
         if (units > 0) {
             load_a(0, 0);
             if (!a.resident) load_b(0, 0);
-            else
-                for (int k = 0; k < chunks; ++k) {
-                    load_b(0, k);
-                    op_b.template store<P == kGradX>(t, b_area + (size_t)k * OpB::kBytes);
-                }
         }
         const int lag = L::kAsyncA ? min(a.stages - 1, 3) : 0;   // chunks of cp.async on their way behind the newest
         int stage = 0, late = 0, unreported = 0;
@@ -494,7 +501,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
                 if constexpr (kMeets)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        load_quad<VEC>(meets[c % kSlots][r >> 1][r & 1], meet + (row0 + 8 * r) * width + f0 + 16 * c,
+                        load_quad<VO>(meets[c % kSlots][r >> 1][r & 1], meet + (row0 + 8 * r) * width + f0 + 16 * c,
                                        row0 + 8 * r < real ? width - f0 - 16 * c : 0);
             };
             if (kMeets && meet)
@@ -544,7 +551,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
                                 times_slope_as<ACT>(g, z);
                                 store_quad<true>((float*)a.out + row * a.ld_gz + f, g, a.ld_gz - f);   // (whole vectors: ld_gz)
                             } else {
-                                store_quad<VEC>((T*)a.out + row * width + f, z, width - f);
+                                store_quad<VO>((T*)a.out + row * width + f, z, width - f);
                             }
                         }
                     }

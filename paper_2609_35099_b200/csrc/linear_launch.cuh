@@ -24,10 +24,10 @@ template <class K> int allow_smem(K kernel, size_t bytes, std::atomic<uint64_t>&
     return E3J_OK;
 }
 
-template <Product P, class T, class G, int NT, int ACT, bool VEC>
+template <Product P, class T, class G, int NT, int ACT, bool VA, bool VO>
 struct Launch {
-    using L = LinTile<P, T, G, NT, VEC>;
-    static constexpr auto kernel = linear_kernel<P, T, G, NT, ACT, VEC>;
+    using L = LinTile<P, T, G, NT, VA, VO>;
+    static constexpr auto kernel = linear_kernel<P, T, G, NT, ACT, VA, VO>;
     static constexpr size_t kStatic = (P == kGradW ? 1024 : NT) * sizeof(float) + 512;
     // Operand stages, and whether all of B's chunks stay in shared memory (with two stages at least).
     static int shape(LinArgs& a, int chunks, size_t& smem) {
@@ -60,16 +60,20 @@ struct Launch {
     }
 };
 
-template <Product P, class T, class G, int ACT = E3J_ACT_NONE> int product(LinArgs& a, bool vector, cudaStream_t st) {
-    const bool narrow = (P == kGradX ? a.n_in : a.n_out) <= 64;
-    if (vector) return narrow ? Launch<P, T, G, 64, ACT, true>::run(a, st) : Launch<P, T, G, 128, ACT, true>::run(a, st);
-    return narrow ? Launch<P, T, G, 64, ACT, false>::run(a, st) : Launch<P, T, G, 128, ACT, false>::run(a, st);
+// Which rows start on 16 bytes: those of A; all others (B's, and but for kGradW those of the results and of what they meet).
+struct Aligned { bool a, others; };
+template <Product P, class T, class G, int ACT = E3J_ACT_NONE> int product(LinArgs& x, Aligned v, cudaStream_t st) {
+    const bool narrow = (P == kGradX ? x.n_in : x.n_out) <= 64;
+    if (v.a && v.others) return narrow ? Launch<P, T, G, 64, ACT, true, true>::run(x, st) : Launch<P, T, G, 128, ACT, true, true>::run(x, st);
+    if (v.a) return narrow ? Launch<P, T, G, 64, ACT, true, false>::run(x, st) : Launch<P, T, G, 128, ACT, true, false>::run(x, st);
+    if (v.others) return narrow ? Launch<P, T, G, 64, ACT, false, true>::run(x, st) : Launch<P, T, G, 128, ACT, false, true>::run(x, st);
+    return narrow ? Launch<P, T, G, 64, ACT, false, false>::run(x, st) : Launch<P, T, G, 128, ACT, false, false>::run(x, st);
 }
-template <Product P, class T, class G> int product_act(LinArgs& a, int act, bool vector, cudaStream_t st) {
-    if (act == E3J_ACT_SILU) return product<P, T, G, E3J_ACT_SILU>(a, vector, st);
-    if (act == E3J_ACT_TANH) return product<P, T, G, E3J_ACT_TANH>(a, vector, st);
-    if (act == E3J_ACT_GELU) return product<P, T, G, E3J_ACT_GELU>(a, vector, st);
-    if constexpr (P == kForward) return product<P, T, G>(a, vector, st);
+template <Product P, class T, class G> int product_act(LinArgs& a, int act, Aligned v, cudaStream_t st) {
+    if (act == E3J_ACT_SILU) return product<P, T, G, E3J_ACT_SILU>(a, v, st);
+    if (act == E3J_ACT_TANH) return product<P, T, G, E3J_ACT_TANH>(a, v, st);
+    if (act == E3J_ACT_GELU) return product<P, T, G, E3J_ACT_GELU>(a, v, st);
+    if constexpr (P == kForward) return product<P, T, G>(a, v, st);
     return E3J_ERR_INVALID_ARG;
 }
 
@@ -77,16 +81,16 @@ template <Product P, class T, class G> int product_act(LinArgs& a, int act, bool
 inline bool whole(const void* p, int64_t ld, size_t size) { return !p || (((uintptr_t)p | (uintptr_t)(ld * size)) & 15u) == 0; }
 
 template <class T> int linear_fwd(LinArgs& a, int act, cudaStream_t st) {
-    const bool vector = whole(a.x, a.n_in, sizeof(T)) && whole(a.W, a.n_out, sizeof(T)) && whole(a.out, a.n_out, sizeof(T)) &&
-                        whole(a.residual, a.n_out, sizeof(T));
-    return product_act<kForward, T, T>(a, act, vector, st);
+    const Aligned v{whole(a.x, a.n_in, sizeof(T)),
+                    whole(a.W, a.n_out, sizeof(T)) && whole(a.out, a.n_out, sizeof(T)) && whole(a.residual, a.n_out, sizeof(T))};
+    return product_act<kForward, T, T>(a, act, v, st);
 }
 
 template <class T, class G> int gradients(LinArgs a, const BwdLayout& L, void* grad_x, void* grad_W, void* grad_b, cudaStream_t st) {
     const bool gz = whole(a.gz, a.ld_gz, sizeof(G));
     if (grad_x) {
         a.out = grad_x;
-        if (int rc = product<kGradX, T, G>(a, gz && whole(a.W, a.n_out, sizeof(T)) && whole(grad_x, a.n_in, sizeof(T)), st)) return rc;
+        if (int rc = product<kGradX, T, G>(a, Aligned{gz, whole(a.W, a.n_out, sizeof(T)) && whole(grad_x, a.n_in, sizeof(T))}, st)) return rc;
     }
     if (!grad_W && !grad_b) return E3J_OK;
     a.ranges = L.ranges;
@@ -94,7 +98,7 @@ template <class T, class G> int gradients(LinArgs a, const BwdLayout& L, void* g
     a.want_sums = grad_b != nullptr;
     a.grad_W = grad_W;
     a.grad_b = grad_b;
-    if (int rc = product<kGradW, T, G>(a, gz && whole(a.x, a.n_in, sizeof(T)), st)) return rc;
+    if (int rc = product<kGradW, T, G>(a, Aligned{whole(a.x, a.n_in, sizeof(T)), gz}, st)) return rc;
     if (L.direct) return E3J_OK;
     return sum_shares<T>(L.ranges, (int64_t)a.n_in * a.n_out, a.n_out, a.shares, (T*)grad_W, (T*)grad_b, st);
 }
@@ -133,8 +137,8 @@ int linear_bwd(LinArgs& a, int act, const BwdLayout& L, void* workspace, void* g
     }
     a.out = workspace;
     a.ld_gz = (int)L.ld_gz;
-    const bool vector = whole(a.x, a.n_in, sizeof(T)) && whole(a.W, a.n_out, sizeof(T)) && whole(a.grad_y, a.n_out, sizeof(T));
-    if (int rc = product_act<kSlope, T, float>(a, act, vector, st)) return rc;
+    const Aligned v{whole(a.x, a.n_in, sizeof(T)), whole(a.W, a.n_out, sizeof(T)) && whole(a.grad_y, a.n_out, sizeof(T))};
+    if (int rc = product_act<kSlope, T, float>(a, act, v, st)) return rc;
     a.gz = workspace;
     return gradients<T, float>(a, L, grad_x, grad_W, grad_b, st);
 }
