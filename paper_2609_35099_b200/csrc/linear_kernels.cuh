@@ -16,7 +16,7 @@
 //
 // Accumulators.  The tensor cores add with truncation, so long chains drift (see radial_gemm.cuh).  Of float32 operands the
 // hi hi products go to one accumulator and the five smaller ones to another (B's hi and mid lie behind one another, so the first
-// two are one instruction of twice the width), and a chain ends after kGroupChunks chunks, 16 additions of hi hi: the epilogue adds groups in
+// two are one instruction of twice the width), and a chain ends after kChainRows rows, 16 additions of hi hi: the epilogue adds groups in
 // float32 registers.
 //
 // Order of a tile's columns.  A quad of lanes reads tensor memory in pieces of 8 columns, two a lane (tcgen05.ld 16x256b).  Columns
@@ -42,8 +42,7 @@ constexpr int lin_threads(int size) { return read_warps(size) * 32 + kRoleThread
 constexpr int kMostStages = 6;
 constexpr int kTileRows = 128;      // accumulator lanes
 constexpr int kChunk = 64;          // contraction elements a chunk
-constexpr int kGroupChunks = 4;     // chunks a chain (float32 sums over rows)
-constexpr int kPanelBytes = 64 * 128;   // 64 rows of a panel
+constexpr int kChainRows = 256;     // rows a chain of sums over rows is long
 
 // ---------------------------------------------------------------- operands
 // Four consecutive elements, `left` of which are there, as they lie in memory.
@@ -255,8 +254,11 @@ template <class T, class G> struct Types<kGradW, T, G> {
 template <Product P, class T, class G, int NT, bool VA, bool VO> struct LinTile {
     using Ty = Types<P, T, G>;
     static constexpr bool kRowSum = P == kGradW;    // contraction over rows: both operands MN-major
-    using OpA = Operand<typename Ty::A, Ty::a_terms, kRowSum ? kChunk : kTileRows, kRowSum ? kTileRows : kChunk, false, VA>;
-    using OpB = Operand<typename Ty::B, Ty::b_terms, P == kGradX ? NT : kChunk, P == kGradX ? kChunk : NT, P != kGradX, VO>;
+    // Sums over rows of float32 take 32 rows at a time: with 64 the loaders' registers do not hold both operands of a chunk, and what
+    // is spilled is waited for (60 000 rows of 128 -> 128: UUU us against VVV).
+    static constexpr int kRows = kRowSum && Ty::a_terms == 3 ? 32 : kChunk;
+    using OpA = Operand<typename Ty::A, Ty::a_terms, kRowSum ? kRows : kTileRows, kRowSum ? kTileRows : kChunk, false, VA>;
+    using OpB = Operand<typename Ty::B, Ty::b_terms, P == kGradX ? NT : kRows, P == kGradX ? kChunk : NT, P != kGradX, VO>;
     static constexpr bool kA_mn = kRowSum, kB_mn = P != kGradX;
     static constexpr int kSets = Ty::a_terms == 3 ? 2 : 1;     // accumulators of a tile
     static constexpr int kColumns = 2 * kSets * NT;            // tensor memory: two tiles
@@ -272,6 +274,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
     using OpA = typename L::OpA;
     using OpB = typename L::OpB;
     constexpr int kTermsA = L::Ty::a_terms, kTermsB = L::Ty::b_terms;
+    constexpr int kChunkRows = L::kRows, kGroupChunks = kChainRows / L::kRows;   // (kGradW)
     extern __shared__ unsigned char raw_smem[];
     __shared__ uint64_t full[kMostStages], empty[kMostStages], tile_full[2], tile_empty[2], drain;
     __shared__ uint32_t tmem_slot;
@@ -308,7 +311,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
     if constexpr (P == kGradW) {
         const int tile = blockIdx.x % (a.n_tiles * a.m_tiles), range = blockIdx.x / (a.n_tiles * a.m_tiles);
         m0 = tile / a.n_tiles * kTileRows;
-        const int64_t all = (real + kChunk - 1) / kChunk;
+        const int64_t all = (real + kChunkRows - 1) / kChunkRows;
         chunk_begin = all * range / a.ranges;
         chunk_end = all * (range + 1) / a.ranges;
         units = (int)((chunk_end - chunk_begin + kGroupChunks - 1) / kGroupChunks);
@@ -348,7 +351,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
         OpA op_a;
         OpB op_b;
         auto with_a = [&](int unit, int chunk, auto&& f) {   // the block of A that a chunk takes
-            if constexpr (P == kGradW) f((const TA*)a.x, (int64_t)a.n_in, (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunk, m0, a.n_in);
+            if constexpr (P == kGradW) f((const TA*)a.x, (int64_t)a.n_in, (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunkRows, m0, a.n_in);
             else if constexpr (P == kGradX) f((const TA*)a.gz, (int64_t)a.ld_gz, (unit0 + unit * unit_step) * kTileRows, chunk * kChunk, a.ld_gz);
             else f((const TA*)a.x, (int64_t)a.n_in, (unit0 + unit * unit_step) * kTileRows, chunk * kChunk, a.n_in);
         };
@@ -357,7 +360,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
                 with_a(unit, chunk, [&](const TA* from, int64_t ld, int64_t row0, int col0, int col_end) { op_a.load(t, from, ld, row0, real, col0, col_end); });
         };
         auto load_b = [&](int unit, int chunk) {
-            if constexpr (P == kGradW) op_b.load(t, (const TB*)a.gz, a.ld_gz, (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunk, real, n0, a.ld_gz);
+            if constexpr (P == kGradW) op_b.load(t, (const TB*)a.gz, a.ld_gz, (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunkRows, real, n0, a.ld_gz);
             else load_w(op_b, t, chunk);
         };
         float2 col_sum[2] = {both(0.f), both(0.f)};   // kGradW: of this thread's four columns of gz, the same in every chunk
@@ -383,7 +386,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
                 unsigned char* const to = smem + (size_t)stage * OpA::kBytes;
                 if constexpr (L::kAsyncA)
                     with_a(unit, chunk, [&](const TA* from, int64_t ld, int64_t row0, int col0, int col_end) {
-                        copy_async<P == kGradW ? kChunk : kTileRows, P == kGradW ? kTileRows : kChunk>(t, umma::smem_addr(to), from, ld, row0, real, col0, col_end);
+                        copy_async<P == kGradW ? kChunkRows : kTileRows, P == kGradW ? kTileRows : kChunk>(t, umma::smem_addr(to), from, ld, row0, real, col0, col_end);
                     });
                 else op_a.store(t, to);
                 if (!a.resident) {
@@ -452,12 +455,12 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
                     if (!(ok = fast::mbar_wait(&full[stage], turn & 1, abort_flag, a.status))) break;
                     umma::fence_after_sync();
                     const uint32_t pa = a_addr + stage * OpA::kBytes, pb = b_addr + (a.resident ? chunk : stage) * OpB::kBytes;
-                    int steps = kChunk / 16;   // those that hold anything
+                    int steps = L::kRows / 16;   // those that hold anything
                     if constexpr (P != kGradW) steps = min(steps, ((P == kGradX ? a.n_out : a.n_in) - chunk * kChunk + 15) / 16);
                     for (int k = 0; k < steps; ++k) {
                         const uint32_t add = chunk > 0 || k > 0;   // (else the accumulators are overwritten)
-                        auto da = [&](int term) { return swizzled_desc(pa + term * OpA::kTermBytes + k * a_step, kPanelBytes, 1024); };
-                        auto db = [&](int term) { return swizzled_desc(pb + term * OpB::kTermBytes + k * b_step, kPanelBytes, 1024); };
+                        auto da = [&](int term) { return swizzled_desc(pa + term * OpA::kTermBytes + k * a_step, L::kRows * 128, 1024); };
+                        auto db = [&](int term) { return swizzled_desc(pb + term * OpB::kTermBytes + k * b_step, L::kRows * 128, 1024); };
                         if constexpr (kTermsA == 3) {
                             mma_bf16(d, da(0), db(0), two, add);         // hi [hi | mid]
                             mma_bf16(d + NT, da(1), db(0), one, 1);
