@@ -324,7 +324,7 @@ NormShape norm_shape(int64_t rows, int n, int size, bool bwd, bool aligned) {
     const int64_t resident = (int64_t)sm_count() * norm_blocks(s.vector ? v : 1, s.each, s.ragged, bwd);
     s.blocks = (int)std::min<int64_t>((rows + per_turn - 1) / per_turn, resident);
     // Few rows, backward: one cluster, whose blocks take up to kClusterTurns turns, and no second kernel for the sums (1201 rows of
-    // 64: 14 us with it, LLL without).
+    // 64: 14.3 us with it, 9.5 without, both bound by the host).
     s.direct = bwd && rows <= kClusterBlocks * kClusterTurns * per_turn;
     if (s.direct) s.blocks = std::min(s.blocks, kClusterBlocks);
     const int step = (int)std::max<int64_t>(v / per_turn, 1);   // (ragged rows: the stride is a multiple of v rows)

@@ -25,6 +25,7 @@ struct LinArgs {
     float* shares;         // kGradW: [ranges][n_in * n_out + n_out]; null: the parameters' gradients are written here
     void *grad_W, *grad_b; // (either may be null: not wanted)
     int ranges, want_sums;
+    int beside;            // kGradW: launched behind kGradX
     int n_tiles;           // tiles of 128 (kGradW: of its two dimensions, n_tiles x m_tiles) or NT columns
     int m_tiles;
     int stages, resident;  // operand stages; B's chunks stay in shared memory
