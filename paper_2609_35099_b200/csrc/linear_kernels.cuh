@@ -16,8 +16,9 @@
 //
 // Accumulators.  The tensor cores add with truncation, so long chains drift (see radial_gemm.cuh).  Of float32 operands the
 // hi hi products go to one accumulator and the five smaller ones to another (B's hi and mid lie behind one another, so the first
-// two are one instruction of twice the width), and a chain ends after kChainRows rows, 16 additions of hi hi: the epilogue adds groups in
-// float32 registers.
+// two are one instruction of twice the width), and a chain ends after kChain of the contraction, 16 additions of hi hi: the readers
+// add the chains in registers, rounding.  Products over up to kLongest columns are one chain of 32 at most (2-norm of the error,
+// normal values: 1.1e-7 with 64, 5e-7 with 512; 4096 would be 4.6e-6).
 //
 // Order of a tile's columns.  A quad of lanes reads tensor memory in pieces of 8 columns, two a lane (tcgen05.ld 16x256b).  Columns
 // of a 16-column group are dealt out so that the two pieces of a lane are four consecutive features: rows leave in 64-byte (float32) or
@@ -42,7 +43,8 @@ constexpr int lin_threads(int size) { return read_warps(size) * 32 + kRoleThread
 constexpr int kMostStages = 6;
 constexpr int kTileRows = 128;      // accumulator lanes
 constexpr int kChunk = 64;          // contraction elements a chunk
-constexpr int kChainRows = 256;     // rows a chain of sums over rows is long
+constexpr int kChain = 256;         // contraction elements a chain is long (sums over rows; LONG products)
+constexpr int kLongest = 512;       // ... of other products
 
 // ---------------------------------------------------------------- operands
 // Four consecutive elements, `left` of which are there, as they lie in memory.
@@ -266,7 +268,8 @@ template <Product P, class T, class G, int NT, bool VA, bool VO> struct LinTile 
     static size_t smem_bytes(int stages, int b_slots) { return 1024 + (size_t)stages * OpA::kBytes + (size_t)b_slots * OpB::kBytes; }
 };
 
-template <Product P, class T, class G, int NT, int ACT, bool VA, bool VO>
+// LONG: the contraction is cut into chains (float32 products over more than kLongest columns).
+template <Product P, class T, class G, int NT, int ACT, bool VA, bool VO, bool LONG>
 __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const __grid_constant__ LinArgs a) {
     using L = LinTile<P, T, G, NT, VA, VO>;
     using TA = typename L::Ty::A;
@@ -274,7 +277,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
     using OpA = typename L::OpA;
     using OpB = typename L::OpB;
     constexpr int kTermsA = L::Ty::a_terms, kTermsB = L::Ty::b_terms;
-    constexpr int kChunkRows = L::kRows, kGroupChunks = kChainRows / L::kRows;   // (kGradW)
+    constexpr int kChunkRows = L::kRows, kGroupChunks = kChain / L::kRows;   // chunks a chain
     extern __shared__ unsigned char raw_smem[];
     __shared__ uint64_t full[kMostStages], empty[kMostStages], tile_full[2], tile_empty[2], drain;
     __shared__ uint32_t tmem_slot;
@@ -307,8 +310,9 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
             bias[threadIdx.x] = a.b && n0 + (int)threadIdx.x < a.n_out ? to_float(((const T*)a.b)[n0 + threadIdx.x]) : 0.f;
     const int64_t real = real_rows(a.rows, a.n_real);
 
-    // ---- what this block does: units (a tile, or for kGradW a group of chunks of one tile) of `chunks` chunks
+    // ---- what this block does: units (a tile, or for kGradW and LONG a chain of one tile) of up to `chunks` chunks
     int units, chunks, m0 = 0;
+    int chains = 1;                            // LONG: units of a tile
     int64_t unit0 = 0, unit_step = 1;          // row tiles of this block
     int64_t chunk_begin = 0, chunk_end = 0;    // kGradW: chunks of rows of this block
     if constexpr (P == kGradW) {
@@ -325,9 +329,17 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
         unit_step = gridDim.x / a.n_tiles;
         units = (int)(tiles > unit0 ? (tiles - unit0 + unit_step - 1) / unit_step : 0);
         chunks = ((P == kGradX ? a.n_out : a.n_in) + kChunk - 1) / kChunk;
+        if constexpr (LONG) {
+            chains = (chunks + kGroupChunks - 1) / kGroupChunks;
+            units *= chains;
+        }
     }
+    // of a unit: its tile's first row, its first chunk
+    auto row_of = [&](int unit) { return (unit0 + (LONG ? unit / chains : unit) * unit_step) * kTileRows; };
+    auto first_chunk = [&](int unit) { return LONG ? unit % chains * kGroupChunks : 0; };
     auto chunks_of = [&](int unit) {
         if constexpr (P == kGradW) return (int)min((int64_t)kGroupChunks, chunk_end - chunk_begin - (int64_t)unit * kGroupChunks);
+        else if constexpr (LONG) return min(kGroupChunks, chunks - first_chunk(unit));
         else return chunks;
     };
     unsigned char* const b_area = smem + (size_t)a.stages * OpA::kBytes;
@@ -355,8 +367,8 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
         OpB op_b;
         auto with_a = [&](int unit, int chunk, auto&& f) {   // the block of A that a chunk takes
             if constexpr (P == kGradW) f((const TA*)a.x, (int64_t)a.n_in, (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunkRows, m0, a.n_in);
-            else if constexpr (P == kGradX) f((const TA*)a.gz, (int64_t)a.ld_gz, (unit0 + unit * unit_step) * kTileRows, chunk * kChunk, a.ld_gz);
-            else f((const TA*)a.x, (int64_t)a.n_in, (unit0 + unit * unit_step) * kTileRows, chunk * kChunk, a.n_in);
+            else if constexpr (P == kGradX) f((const TA*)a.gz, (int64_t)a.ld_gz, row_of(unit), (first_chunk(unit) + chunk) * kChunk, a.ld_gz);
+            else f((const TA*)a.x, (int64_t)a.n_in, row_of(unit), (first_chunk(unit) + chunk) * kChunk, a.n_in);
         };
         auto load_a = [&](int unit, int chunk) {
             if constexpr (!L::kAsyncA)
@@ -364,7 +376,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
         };
         auto load_b = [&](int unit, int chunk) {
             if constexpr (P == kGradW) op_b.load(t, (const TB*)a.gz, a.ld_gz, (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunkRows, real, n0, a.ld_gz);
-            else load_w(op_b, t, chunk);
+            else load_w(op_b, t, first_chunk(unit) + chunk);
         };
         float2 col_sum[2] = {both(0.f), both(0.f)};   // kGradW: of this thread's four columns of gz, the same in every chunk
         if (units > 0) {
@@ -457,9 +469,9 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
                 for (int chunk = 0; chunk < n_chunks; ++chunk) {
                     if (!(ok = fast::mbar_wait(&full[stage], turn & 1, abort_flag, a.status))) break;
                     umma::fence_after_sync();
-                    const uint32_t pa = a_addr + stage * OpA::kBytes, pb = b_addr + (a.resident ? chunk : stage) * OpB::kBytes;
+                    const uint32_t pa = a_addr + stage * OpA::kBytes, pb = b_addr + (a.resident ? first_chunk(unit) + chunk : stage) * OpB::kBytes;
                     int steps = L::kRows / 16;   // those that hold anything
-                    if constexpr (P != kGradW) steps = min(steps, ((P == kGradX ? a.n_out : a.n_in) - chunk * kChunk + 15) / 16);
+                    if constexpr (P != kGradW) steps = min(steps, ((P == kGradX ? a.n_out : a.n_in) - (first_chunk(unit) + chunk) * kChunk + 15) / 16);
                     for (int k = 0; k < steps; ++k) {
                         const uint32_t add = chunk > 0 || k > 0;   // (else the accumulators are overwritten)
                         auto da = [&](int term) { return swizzled_desc(pa + term * OpA::kTermBytes + k * a_step, L::kRows * 128, 1024); };
@@ -489,9 +501,10 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
     } else {
         // ------------------------------------------------ readers: accumulators -> registers -> memory
         const int first = (warp >> 2) * kWarpColumns, quarter = warp & 3;   // 32 rows and kWarpColumns columns
-        Quads sums[P == kGradW ? kWarpColumns / 8 : 1];
+        constexpr int kSums = P == kGradW || LONG ? kWarpColumns / 8 : 1;
+        Quads sums[kSums];
 #pragma unroll
-        for (int i = 0; i < (P == kGradW ? kWarpColumns / 8 : 1) * 4; ++i) sums[i >> 2].p[i >> 1 & 1][i & 1] = both(0.f);
+        for (int i = 0; i < kSums * 4; ++i) sums[i >> 2].p[i >> 1 & 1][i & 1] = both(0.f);
         // What the results meet in memory, residual or grad_y, is fetched before the tile is waited for: kSlots groups of 16 columns
         // (as many as the registers hold), the others as these become free.
         constexpr bool kMeets = P == kForward || P == kSlope;
@@ -502,7 +515,8 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
         const T* const meet = (const T*)(P == kForward ? a.residual : a.grad_y);
         for (int unit = 0; unit < units; ++unit) {
             const int set = unit & 1;
-            const int64_t row0 = (unit0 + unit * unit_step) * kTileRows + quarter * 32 + lane / 4;
+            const int64_t row0 = row_of(unit) + quarter * 32 + lane / 4;
+            const bool whole = !LONG || (unit + 1) % chains == 0;   // this unit finishes the tile
             auto fetch = [&](int c) {
                 if constexpr (kMeets)
 #pragma unroll
@@ -510,7 +524,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
                         load_quad<VO>(meets[c % kSlots][r >> 1][r & 1], meet + (row0 + 8 * r) * width + f0 + 16 * c,
                                        row0 + 8 * r < real ? width - f0 - 16 * c : 0);
             };
-            if (kMeets && meet)
+            if (kMeets && meet && whole)
 #pragma unroll
                 for (int c = 0; c < kSlots; ++c) fetch(c);
             if (!fast::mbar_wait(&tile_full[set], (unit >> 1) & 1, abort_flag, a.status)) break;
@@ -533,6 +547,13 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
                         add_quads(v, u);
                     } else {
                         umma::tmem_ld_wait();
+                    }
+                    if constexpr (LONG) {
+                        add_quads(sums[c * 2 + h], v);
+                        if (!whole) continue;
+                        v = sums[c * 2 + h];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sums[c * 2 + h].p[i >> 1][i & 1] = both(0.f);
                     }
                     if constexpr (P == kGradW) {
                         add_quads(sums[c * 2 + h], v);
@@ -562,7 +583,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
                         }
                     }
                 }
-                if (kMeets && meet && c + kSlots < kGroups) fetch(c + kSlots);
+                if (kMeets && meet && whole && c + kSlots < kGroups) fetch(c + kSlots);
             }
             umma::fence_before_sync();
             __syncwarp();

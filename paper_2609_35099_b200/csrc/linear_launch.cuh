@@ -24,10 +24,10 @@ template <class K> int allow_smem(K kernel, size_t bytes, std::atomic<uint64_t>&
     return E3J_OK;
 }
 
-template <Product P, class T, class G, int NT, int ACT, bool VA, bool VO>
+template <Product P, class T, class G, int NT, int ACT, bool VA, bool VO, bool LONG = false>
 struct Launch {
     using L = LinTile<P, T, G, NT, VA, VO>;
-    static constexpr auto kernel = linear_kernel<P, T, G, NT, ACT, VA, VO>;
+    static constexpr auto kernel = linear_kernel<P, T, G, NT, ACT, VA, VO, LONG>;
     static constexpr size_t kStatic = (P == kGradW ? 1024 : NT) * sizeof(float) + 512;
     // Operand stages, and whether all of B's chunks stay in shared memory (with two stages at least).
     static int shape(LinArgs& a, int chunks, size_t& smem) {
@@ -67,6 +67,9 @@ template <Product P, class T, class G, int ACT = E3J_ACT_NONE> int product(LinAr
     // forward: 14.9 us with tiles of 128, 11.6 so).  kGradW: as the rows' ranges were laid out (bwd_layout).
     const int columns = P == kGradX ? x.n_in : x.n_out;
     const bool narrow = columns <= 64 || (P != kGradW && (x.rows + kTileRows - 1) / kTileRows * ((columns + 63) / 64) <= sm_count());
+    if constexpr (P != kGradW && sizeof(T) == 4)   // (tiles of 64: the sums of the chains are registers)
+        if ((P == kGradX ? x.n_out : x.n_in) > kLongest)
+            return v.a && v.others ? Launch<P, T, G, 64, ACT, true, true, true>::run(x, st) : Launch<P, T, G, 64, ACT, false, false, true>::run(x, st);
     if (v.a && v.others) return narrow ? Launch<P, T, G, 64, ACT, true, true>::run(x, st) : Launch<P, T, G, 128, ACT, true, true>::run(x, st);
     if (v.a) return narrow ? Launch<P, T, G, 64, ACT, true, false>::run(x, st) : Launch<P, T, G, 128, ACT, true, false>::run(x, st);
     if (v.others) return narrow ? Launch<P, T, G, 64, ACT, false, true>::run(x, st) : Launch<P, T, G, 128, ACT, false, true>::run(x, st);

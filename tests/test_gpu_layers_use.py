@@ -300,3 +300,19 @@ def test_refusals():
     big, g = torch.randn(5000, 64, device="cuda"), torch.randn(5000, 64, device="cuda")
     with pytest.raises(ValueError, match="workspace"):
         e3j.e3j_linear_bwd(big, torch.randn(64, 64, device="cuda"), None, g, workspace=torch.empty(100, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", [(300, 1030, 70), (130, 70, 1030), (200, 4096, 100), (150, 600, 513)])
+def test_long_contractions_keep_float32_accuracy(rows, n_in, n_out):
+    """Values of one sign, for which every addition of the tensor cores cuts off in the same direction: a chain is 16 of them, each up to 2 u
+    of a partial sum that grows evenly (so 16 u on average over the chain), chains and terms are rounded: below 32 u = 2e-6 of
+    the result, against 4096 / 16 * u = 1.5e-5 in one chain."""
+    x, W, g = (torch.rand(*s, device="cuda") for s in ((rows, n_in), (n_in, n_out), (rows, n_out)))
+    for got, want in ((e3j.e3j_linear_fwd(x, W), x.double() @ W.double()),
+                      (e3j.e3j_linear_bwd(x, W, None, g, grad_W=False, grad_b=False)[0], g.double() @ W.double().T)):
+        assert ((got.double() - want).abs() / want).max() <= 2e-6
+    (xs, x_), (Ws, W_), (bs, b_), (gs, g_) = [(t.cuda(), t.double().numpy()) for t in (torch.randn(rows, n_in), torch.randn(n_in, n_out) / n_in ** 0.5, torch.randn(n_out), torch.randn(rows, n_out))]
+    ref.assert_within(e3j.e3j_linear_fwd(xs, Ws, bs, gs, SILU), *ref.linear_fwd(x_, W_, b_, g_, "silu", 2.0 ** -24), "y")
+    want, bounds = ref.linear_bwd(x_, W_, b_, g_, "gelu", 2.0 ** -24)
+    for t, v, e in zip(e3j.e3j_linear_bwd(xs, Ws, bs, gs, GELU), want, bounds):
+        ref.assert_within(t, v, e)
