@@ -315,7 +315,7 @@ int e3j_conv_radial_bwd(const e3j_plan* plan, int64_t n_nodes, int64_t n_edges, 
  * stored.  Tensors are contiguous, row after row, and need only their natural alignment (4 or 2 bytes; rows that start on 16
  * bytes are faster).  An input must not overlap an output.
  *   n_real: DEVICE word with the number of real rows of a padded list (rowptr[n_nodes] of e3j_graph_prepare_padded), or NULL: all
- *   rows are real.  Nothing of the rows behind it is read; their rows of y and grad_x are zeros and the parameters'
+ *   rows are real.  What the rows behind it hold does not matter; their rows of y and grad_x are zeros and the parameters'
  *   gradients leave them out.  Values below 0 count as 0, above `rows` as `rows`.
  * Activations: y = z, z / (1 + exp(-z)), tanh(z), z (1 + erf(z / sqrt 2)) / 2.
  * Results are bit-identical from run to run.  */
@@ -328,7 +328,7 @@ int e3j_conv_radial_bwd(const e3j_plan* plan, int64_t n_nodes, int64_t n_edges, 
 
 /* Linear layer: y = act(x W + b) + residual with x [rows, n_in], W [n_in, n_out], b [n_out] or NULL, residual [rows, n_out] or
  * NULL, y [rows, n_out]; widths from 1 to 4096.  The products run on the tensor cores with float32 accuracy for float32 tensors (each
- * as the sum of three bfloat16 terms); a row with an infinity or a NaN in x comes out as NaN.
+ * as the sum of three bfloat16 terms); a row with an infinity or a NaN in x comes out as NaN, and so does a column of such a W.
  * Backward: gz = grad_y act'(x W + b), formed again from x, W and b (the forward keeps nothing); grad_x = gz W^T, grad_W = x^T gz,
  * grad_b = sum over rows of gz; the residual's gradient is grad_y itself.  Any of grad_x, grad_W, grad_b may be NULL (not wanted).
  * Workspace: 256-byte aligned, e3j_linear_bwd_workspace_bytes() (0: none is needed, NULL will do); calls that overlap on the GPU must

@@ -1,5 +1,6 @@
 // Between the linear layer's C entry points (linear.cu) and its launches (linear_f32.cu, linear_bf16.cu).
 #pragma once
+#include <cuda.h>   // CUtensorMap
 #include <cuda_runtime.h>
 
 #include <cstddef>
@@ -15,6 +16,8 @@ enum Product { kForward, kSlope, kGradX, kGradW };
 // kGradW    shares of x^T gz and of the column sums of gz, one a range of rows
 
 struct LinArgs {
+    CUtensorMap map_a;     // boxes of 128 rows x 64 columns of A, where `boxes` is set
+    int boxes;
     int64_t rows;
     int n_in, n_out;
     const int32_t* n_real;

@@ -25,7 +25,8 @@
 // 32-byte (bfloat16) runs a quad, whole sectors, without a detour through shared memory.  (column_of)
 //
 // A block is one per SM and has three roles: eight warps fetch, split and store operands (one chunk in registers ahead; bfloat16 rows
-// that start on 16 bytes go to shared memory by cp.async, up to four chunks ahead), one issues the tensor-core instructions, eight
+// that start on 16 bytes go to shared memory by cp.async, up to four chunks ahead, or in large calls as boxes of a tensor map, which one
+// thread asks for, as many ahead as there are stages), one issues the tensor-core instructions, eight
 // read accumulators and finish tiles.  Operand stages and two accumulator sets stand between them.  As one role of 256 threads
 // that took turns, two blocks an SM, 160 900 x 64 -> 64 float32 took 25.7 us instead of 22.4.  Waits are bounded (fast::mbar_wait).
 #pragma once
@@ -228,6 +229,11 @@ __device__ __forceinline__ void copy_async(int t, uint32_t image, const bf16* fr
                      "r"(there ? 16 : 0) : "memory");
     }
 }
+// A box of a tensor map with the 128-byte swizzle into an image; x a multiple of 8 columns.
+__device__ __forceinline__ void load_box(uint32_t image, const CUtensorMap* map, int x, int y, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(image), "l"(map), "r"(x), "r"(y), "r"(fast::smem_u32(bar)) : "memory");
+}
 __device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 // all but the newest `n` groups have arrived
 __device__ __forceinline__ void async_wait(int n) {
@@ -264,7 +270,8 @@ template <Product P, class T, class G, int NT, bool VA, bool VO> struct LinTile 
     static constexpr bool kA_mn = kRowSum, kB_mn = P != kGradX;
     static constexpr int kSets = Ty::a_terms == 3 ? 2 : 1;     // accumulators of a tile
     static constexpr int kColumns = 2 * kSets * NT;            // tensor memory: two tiles
-    static constexpr bool kAsyncA = VA && sizeof(typename Ty::A) == 2;   // A by cp.async
+    static constexpr bool kAsyncA = VA && sizeof(typename Ty::A) == 2;   // A by cp.async ...
+    static constexpr bool kBoxes = kAsyncA && !kRowSum;                  // ... or by tiled bulk copies (LinArgs::boxes)
     static size_t smem_bytes(int stages, int b_slots) { return 1024 + (size_t)stages * OpA::kBytes + (size_t)b_slots * OpB::kBytes; }
 };
 
@@ -291,7 +298,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
     constexpr int kWarpColumns = NT / (kReaders / 4);   // of a reading warp
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kMostStages; ++i) { fast::mbar_init(&full[i], kLoaders); fast::mbar_init(&empty[i], 1); }
+        for (int i = 0; i < kMostStages; ++i) { fast::mbar_init(&full[i], L::kBoxes && a.boxes ? 1 : kLoaders); fast::mbar_init(&empty[i], 1); }
         for (int i = 0; i < 2; ++i) { fast::mbar_init(&tile_full[i], 1); fast::mbar_init(&tile_empty[i], kReaders); }
         fast::mbar_init(&drain, 1);
         abort_word = drain_word = 0;
@@ -360,9 +367,30 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
     umma::fence_after_sync();
     const uint32_t tmem = tmem_slot;
 
+    // A as whole boxes, one thread's work; rows behind the last real one come along, and their results go nowhere
+    auto fetch_boxes = [&] {
+        int stage = 0;
+        uint32_t turn = 0;
+        bool ok = true;
+        for (int unit = 0; ok && unit < units; ++unit)
+            for (int chunk = 0; chunk < chunks; ++chunk) {
+                if (turn > 0 && !(ok = fast::mbar_wait(&empty[stage], (turn - 1) & 1, abort_flag, a.status))) break;
+                fast::mbar_arrive_expect_tx(&full[stage], OpA::kBytes);
+                load_box(umma::smem_addr(smem) + stage * OpA::kBytes, &a.map_a, chunk * kChunk, (int)row_of(unit), &full[stage]);
+                if (++stage == a.stages) { stage = 0; ++turn; }
+            }
+        if (!ok)   // a wait ran out: the copies on their way arrive before the block goes
+            for (int i = 0; i < a.stages; ++i)
+                if (turn > 0 || i < stage) fast::mbar_wait(&full[i], (i < stage ? turn : turn - 1) & 1, &drain_word, a.status);
+    };
+
     if (warp >= kReaders && warp < kIssuer) {
         // ------------------------------------------------ loaders: memory -> terms -> stages
         const int t = threadIdx.x - kReaders * 32;
+        float2 col_sum[2] = {both(0.f), both(0.f)};   // kGradW: of this thread's four columns of gz, the same in every chunk
+        if (L::kBoxes && a.boxes) {
+            if (warp == kReaders && lane == 0) fetch_boxes();
+        } else {
         OpA op_a;
         OpB op_b;
         auto with_a = [&](int unit, int chunk, auto&& f) {   // the block of A that a chunk takes
@@ -378,7 +406,6 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
             if constexpr (P == kGradW) op_b.load(t, (const TB*)a.gz, a.ld_gz, (chunk_begin + (int64_t)unit * kGroupChunks + chunk) * kChunkRows, real, n0, a.ld_gz);
             else load_w(op_b, t, first_chunk(unit) + chunk);
         };
-        float2 col_sum[2] = {both(0.f), both(0.f)};   // kGradW: of this thread's four columns of gz, the same in every chunk
         if (units > 0) {
             load_a(0, 0);
             if (!a.resident) load_b(0, 0);
@@ -427,6 +454,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
         }
         if constexpr (L::kAsyncA) async_wait(0);
         while (ok && unreported > 0) report();
+        }
         if constexpr (P == kGradW) {
             if (a.want_sums && m0 == 0) {
                 const int across = t % OpB::kAcross, group = t / OpB::kAcross;

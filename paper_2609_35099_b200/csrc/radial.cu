@@ -9,6 +9,7 @@
 #include "fast/fast_radial.cuh"
 #include "fast_registry.hpp"
 #include "radial_gemm.cuh"
+#include "tensor_map.hpp"
 
 namespace e3j {
 
@@ -53,20 +54,6 @@ int launch_gemm(const Prob& prob, dim3 grid, cudaStream_t st, int resident_chunk
 // Tensor map of a row-major float32 matrix [rows][cols] with `pitch` floats between rows, fetched in boxes of
 // box_cols x box_rows.  False where the matrix does not meet the copy engine's alignment rules (16-byte aligned
 // base and rows) or the driver has no encoder.
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiled tensor_map_encoder() {
-    static const EncodeTiled fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return reinterpret_cast<EncodeTiled>(p);
-    }();
-    return fn;
-}
 bool make_map(CUtensorMap* map, const float* base, int64_t rows, int64_t cols, int64_t pitch, int box_cols, int box_rows,
               bool swizzle128) {
     const EncodeTiled encode = tensor_map_encoder();
