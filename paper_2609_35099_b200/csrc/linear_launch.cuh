@@ -79,10 +79,13 @@ struct Launch {
 // Which rows start on 16 bytes: those of A; all others (B's, and but for kGradW those of the results and of what they meet).
 struct Aligned { bool a, others; };
 template <Product P, class T, class G, int ACT = E3J_ACT_NONE> int product(LinArgs& x, Aligned v, cudaStream_t st) {
-    // Tiles of 64 columns where there are no more, and where all of them have an SM of their own (1218 rows of 336 -> 328 float32
-    // forward: 14.9 us with tiles of 128, 11.6 so).  kGradW: as the rows' ranges were laid out (bwd_layout).
     const int columns = P == kGradX ? x.n_in : x.n_out;
-    const bool narrow = columns <= 64 || (P != kGradW && (x.rows + kTileRows - 1) / kTileRows * ((columns + 63) / 64) <= sm_count());
+    // Tiles of 64 columns instead of 128: where there are no more columns; with float32 where they leave fewer columns of the tiles empty
+    // (41 003 rows, 97 -> 161: x W and the slope 48 us with tiles of 128, 38 so; 60 000 x 128 -> 128 21.3 and 26.3, so not elsewhere;
+    // sums over rows, 38 and 44, not either); and where every one of them has an SM of its own (1218 rows of 336 -> 328 float32
+    // forward: 14.9 us with tiles of 128, 11.6 so).
+    const bool fewer = P != kGradW && sizeof(T) == 4 && (columns - 1) % 128 < 64;
+    const bool narrow = columns <= 64 || fewer || (P != kGradW && (x.rows + kTileRows - 1) / kTileRows * ((columns + 63) / 64) <= sm_count());
     if constexpr (P != kGradW && sizeof(T) == 4)   // (tiles of 64: the sums of the chains are registers)
         if ((P == kGradX ? x.n_out : x.n_in) > kLongest)
             return v.a && v.others ? Launch<P, T, G, 64, ACT, true, true, true>::run(x, st) : Launch<P, T, G, 64, ACT, false, false, true>::run(x, st);
