@@ -79,9 +79,9 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) linear_bwd_narrow_kernel(co
         abort_word = drain_word = 0;
         fast::mbar_fence_init();
     }
-    if (warp == kWorkWarps) umma::tmem_alloc(&tmem_slot, 512);
     fast::grid_dependency_wait();
     fast::grid_dependency_trigger();
+    if (warp == kWorkWarps) umma::tmem_alloc(&tmem_slot, 512);   // (behind the wait: see linear_kernel)
     const int64_t real = real_rows(a.rows, a.n_real);
     const int64_t row_tiles = (real + kTileRows - 1) / kTileRows;
     const int tiles = (int)(row_tiles > blockIdx.x ? (row_tiles - blockIdx.x + gridDim.x - 1) / gridDim.x : 0);   // of this block

@@ -304,12 +304,13 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
         abort_word = drain_word = 0;
         fast::mbar_fence_init();
     }
-    if (warp == kIssuer) umma::tmem_alloc(&tmem_slot, L::kColumns);
     // Sums over rows that follow grad_x's product do not need it, and what came before that product is over when all of its blocks have
     // got as far as their trigger: they run beside it, and only their end comes after its end.
     const bool beside = P == kGradW && a.beside;
     if (!beside) fast::grid_dependency_wait();
     fast::grid_dependency_trigger();
+    // (a block that waits for another kernel holds no tensor memory, which a block of that kernel may be waiting for)
+    if (warp == kIssuer) umma::tmem_alloc(&tmem_slot, L::kColumns);
     const int nt = blockIdx.x % a.n_tiles;
     const int n0 = nt * NT;
     if constexpr (P == kForward || P == kSlope)
@@ -634,11 +635,11 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
                     }
         }
     }
-    if (beside) fast::grid_dependency_wait();
     umma::fence_before_sync();
     __syncthreads();
     umma::fence_after_sync();
     if (warp == kIssuer) umma::tmem_dealloc(tmem, L::kColumns);
+    if (beside) fast::grid_dependency_wait();
 }
 
 }  // namespace layer

@@ -316,3 +316,24 @@ def test_long_contractions_keep_float32_accuracy(rows, n_in, n_out):
     want, bounds = ref.linear_bwd(x_, W_, b_, g_, "gelu", 2.0 ** -24)
     for t, v, e in zip(e3j.e3j_linear_bwd(xs, Ws, bs, gs, GELU), want, bounds):
         ref.assert_within(t, v, e)
+
+
+@pytest.mark.parametrize("n_in,n_out,act", [(128, 96, SILU), (8, 64, 0), (200, 200, 0), (72, 130, GELU)])
+def test_large_padded_calls_in_bfloat16(n_in, n_out, act):
+    """Large enough for operands to come as boxes, NaN behind the last real row (inside a tile): the rows of the short call to the
+    bits, and the gradients within their bounds."""
+    rows, real = 61_003, 40_007
+    x, W, b, r = ((torch.randn(*s, device="cuda") * k).bfloat16() for s, k in (((rows, n_in), 1), ((n_in, n_out), n_in ** -0.5), ((n_out,), 1), ((rows, n_out), 1)))
+    x[real:], r[real:] = float("nan"), float("nan")
+    count = torch.tensor([real], dtype=torch.int32, device="cuda")
+    y = e3j.e3j_linear_fwd(x, W, b, r, act, n_real=count)
+    assert (y[real:] == 0).all() and torch.equal(y[:real], e3j.e3j_linear_fwd(x[:real], W, b, r[:real], act))
+    got = e3j.e3j_linear_bwd(x, W, b, r, act, n_real=count)
+    assert (got[0][real:] == 0).all()
+    name = {0: "none", 1: "silu", 3: "gelu"}[act]
+    x_, W_, b_, g_ = (t.double().cpu().numpy() for t in (x[:real], W, b, r[:real]))
+    ref.assert_within(y[:real], *ref.linear_fwd(x_, W_, b_, g_, name, 2.0 ** -8))
+    want, bounds = ref.linear_bwd(x_, W_, b_, g_, name, 2.0 ** -8)
+    for t, v, e in zip((got[0][:real], *got[1:]), want, bounds):
+        ref.assert_within(t, v, e)
+    assert e3j.e3j_linear_status() == 0
