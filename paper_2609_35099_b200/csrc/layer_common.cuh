@@ -157,13 +157,16 @@ __device__ __forceinline__ float2 normal_tail(float2 z, float2& e) {
     poly = __ffma2_rn(poly, t, both(0.5f * 0.254829592f));
     return __fmul2_rn(__fmul2_rn(poly, t), e);
 }
+// |z| where Phi(-|z|) is not 0 in float32; beyond, for positive z, something finite: infinity times 0 is not what is left of
+// infinity (of -infinity it is: the definition has that product too)
+__device__ __forceinline__ float size(float z) { return fmaxf(fminf(z, 20.f), -z); }
 template <int ACT> __device__ __forceinline__ float2 activation(float2 z) {
     if constexpr (ACT == E3J_ACT_SILU) return __fmul2_rn(z, logistic(z));
     else if constexpr (ACT == E3J_ACT_TANH) return make_float2(tanhf(z.x), tanhf(z.y));
     else if constexpr (ACT == E3J_ACT_GELU) {   // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
         float2 e;
         const float2 tail = normal_tail(z, e);
-        return make_float2(fmaf(-fabsf(z.x), tail.x, fmaxf(z.x, 0.f)), fmaf(-fabsf(z.y), tail.y, fmaxf(z.y, 0.f)));
+        return make_float2(fmaf(-size(z.x), tail.x, fmaxf(z.x, 0.f)), fmaf(-size(z.y), tail.y, fmaxf(z.y, 0.f)));
     } else return z;
 }
 template <int ACT> __device__ __forceinline__ float2 slope(float2 z) {
