@@ -317,8 +317,9 @@ int e3j_conv_radial_bwd(const e3j_plan* plan, int64_t n_nodes, int64_t n_edges, 
  *   n_real: DEVICE word with the number of real rows of a padded list (rowptr[n_nodes] of e3j_graph_prepare_padded), or NULL: all
  *   rows are real.  What the rows behind it hold does not matter; their rows of y and grad_x are zeros and the parameters'
  *   gradients leave them out.  Values below 0 count as 0, above `rows` as `rows`.
- * Activations: y = z, z / (1 + exp(-z)), tanh(z), z (1 + erf(z / sqrt 2)) / 2; of infinite z what these formulas give (NaN for the second
- * and the fourth of -infinity).
+ * Activations: y = z, z / (1 + exp(-z)), tanh(z), z (1 + erf(z / sqrt 2)) / 2; of infinite z
+ * infinity (tanh: 1), and of -infinity -infinity, NaN (-infinity / infinity), -1 and 0.  Slopes at infinite z are NaN but for the first
+ * and the third.
  * Results are bit-identical from run to run.  */
 #define E3J_F32 0
 #define E3J_BF16 1

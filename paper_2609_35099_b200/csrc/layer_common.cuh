@@ -143,13 +143,15 @@ __device__ __forceinline__ float2 logistic(float2 z) {
     const float2 d = __fadd2_rn(make_float2(fast_exp2(x.x), fast_exp2(x.y)), both(1.f));
     return make_float2(fast_reciprocal(d.x), fast_reciprocal(d.y));
 }
-// Normal distribution: Phi(-|z|), and e = exp(-z^2 / 2).  The rational approximation of Hastings for erf (Abramowitz and Stegun
-// 7.1.26), 1 - (a1 t + .. + a5 t^5) exp(-x^2) with t = 1 / (1 + p x) and x = |z| / sqrt 2, which is within 1.5e-7 (2.5 half steps of
-// float32 at 1).  78 000 x 512 -> 512 bfloat16 with GELU is bound by instructions: forward 98 us, with the same
-// element by element 106.
-__device__ __forceinline__ float2 normal_tail(float2 z, float2& e) {
+// Normal distribution: Phi(-|z|), and e = exp(-z^2 / 2), for bfloat16 results.  The rational approximation of Hastings for erf (Abramowitz
+// and Stegun 7.1.26), 1 - (a1 t + .. + a5 t^5) exp(-x^2) with t = 1 / (1 + p x) and x = |z| / sqrt 2, which is within 1.5e-7: far
+// below half a step of bfloat16, but 2.5 half steps of float32 at 1, and more of what is smaller.
+__device__ __forceinline__ float2 normal_exp(float2 z) {
     const float2 x = __fmul2_rn(__fmul2_rn(z, z), both(-0.5f * kLog2e));
-    e = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+    return make_float2(fast_exp2(x.x), fast_exp2(x.y));
+}
+__device__ __forceinline__ float2 normal_tail(float2 z, float2& e) {
+    e = normal_exp(z);
     const float2 t = make_float2(fast_reciprocal(fmaf(0.23164189f, fabsf(z.x), 1.f)), fast_reciprocal(fmaf(0.23164189f, fabsf(z.y), 1.f)));
     float2 poly = __ffma2_rn(both(0.5f * 1.061405429f), t, both(0.5f * -1.453152027f));
     poly = __ffma2_rn(poly, t, both(0.5f * 1.421413741f));
@@ -157,25 +159,67 @@ __device__ __forceinline__ float2 normal_tail(float2 z, float2& e) {
     poly = __ffma2_rn(poly, t, both(0.5f * 0.254829592f));
     return __fmul2_rn(__fmul2_rn(poly, t), e);
 }
-// |z| where Phi(-|z|) is not 0 in float32; beyond, for positive z, something finite: infinity times 0 is not what is left of
-// infinity (of -infinity it is: the definition has that product too)
-__device__ __forceinline__ float size(float z) { return fmaxf(fminf(z, 20.f), -z); }
-template <int ACT> __device__ __forceinline__ float2 activation(float2 z) {
+// The same for float32 results, by two least-maximum fits of our own in float64 (weighted least squares, the weights moved to where
+// the error is largest): near 0, |z| < kNearZero, Phi(z) - 1/2 = z Q(z^2) (relative error 3e-9), beyond it
+// Phi(-|z|) = e t P(t), t = 1 / (1 + 0.4 |z|) (6e-8 of the tail).  Both are evaluated, the caller takes one.  2-norm of GELU's error over
+// normal values 3.5e-8 (z (1 + erf(z / sqrt 2)) / 2 in float32: 3.8e-8; by Hastings 9e-8, 22e-8 for values a tenth of that).
+constexpr float kNearZero = 1.5f;
+__device__ __forceinline__ void normal_parts(float2 z, float2& e, float2& middle, float2& tail) {
+    e = normal_exp(z);
+    const float2 s = __fmul2_rn(z, z);
+    float2 q = __ffma2_rn(both(4.1385521853953833e-07f), s, both(-8.733937647775747e-06f));
+    q = __ffma2_rn(q, s, both(1.1439632362453267e-04f));
+    q = __ffma2_rn(q, s, both(-1.1865355772897601e-03f));
+    q = __ffma2_rn(q, s, both(9.973266161978245e-03f));
+    q = __ffma2_rn(q, s, both(-6.649033725261688e-02f));
+    middle = __ffma2_rn(q, s, both(0.3989422917366028f));   // Q: (Phi(z) - 1/2) / z
+    const float2 t = make_float2(fast_reciprocal(fmaf(0.4f, fabsf(z.x), 1.f)), fast_reciprocal(fmaf(0.4f, fabsf(z.y), 1.f)));
+    float2 p = __ffma2_rn(both(0.06783036142587662f), t, both(-0.18598994612693787f));
+    p = __ffma2_rn(p, t, both(0.1051749661564827f));
+    p = __ffma2_rn(p, t, both(0.05552689731121063f));
+    p = __ffma2_rn(p, t, both(0.13903166353702545f));
+    p = __ffma2_rn(p, t, both(0.15909291803836823f));
+    p = __ffma2_rn(p, t, both(0.1595963090658188f));
+    tail = __fmul2_rn(__fmul2_rn(p, t), e);
+}
+// |z|, but finite: beyond 20 Phi(-|z|) is 0 in float32, and infinity times 0 is not what GELU leaves of infinity
+__device__ __forceinline__ float size(float z) { return fminf(fabsf(z), 20.f); }
+// GELU and its slope (of one element) from those parts: near 0 z / 2 + z (z Q), elsewhere as above; Phi(z) + z phi(z).
+__device__ __forceinline__ float2 gelu_of(float2 z, float2 middle, float2 tail) {
+    const float2 near = __ffma2_rn(z, __fmul2_rn(z, middle), __fmul2_rn(z, both(0.5f)));
+    return make_float2(fabsf(z.x) < kNearZero ? near.x : fmaf(-size(z.x), tail.x, fmaxf(z.x, 0.f)),
+                       fabsf(z.y) < kNearZero ? near.y : fmaf(-size(z.y), tail.y, fmaxf(z.y, 0.f)));
+}
+__device__ __forceinline__ float gelu_slope_of(float z, float e, float middle, float tail) {
+    const float density = e * 0.39894228f;
+    const bool near = fabsf(z) < kNearZero;
+    return fmaf(z, near ? middle + density : density, near ? 0.5f : z > 0.f ? 1.f - tail : tail);
+}
+// FINE: for float32 results (GELU alone has two forms)
+template <int ACT, bool FINE> __device__ __forceinline__ float2 activation(float2 z) {
     if constexpr (ACT == E3J_ACT_SILU) return __fmul2_rn(z, logistic(z));
     else if constexpr (ACT == E3J_ACT_TANH) return make_float2(tanhf(z.x), tanhf(z.y));
-    else if constexpr (ACT == E3J_ACT_GELU) {   // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
+    else if constexpr (ACT == E3J_ACT_GELU && FINE) {
+        float2 e, middle, tail;
+        normal_parts(z, e, middle, tail);
+        return gelu_of(z, middle, tail);
+    } else if constexpr (ACT == E3J_ACT_GELU) {   // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
         float2 e;
         const float2 tail = normal_tail(z, e);
         return make_float2(fmaf(-size(z.x), tail.x, fmaxf(z.x, 0.f)), fmaf(-size(z.y), tail.y, fmaxf(z.y, 0.f)));
     } else return z;
 }
-template <int ACT> __device__ __forceinline__ float2 slope(float2 z) {
+template <int ACT, bool FINE> __device__ __forceinline__ float2 slope(float2 z) {
     if constexpr (ACT == E3J_ACT_SILU) {   // s (1 + z (1 - s))
         const float2 s = logistic(z);
         return __fmul2_rn(s, __ffma2_rn(z, __ffma2_rn(s, both(-1.f), both(1.f)), both(1.f)));
     } else if constexpr (ACT == E3J_ACT_TANH) {
         const float2 t = make_float2(tanhf(z.x), tanhf(z.y));
         return __ffma2_rn(__fmul2_rn(t, both(-1.f)), t, both(1.f));
+    } else if constexpr (ACT == E3J_ACT_GELU && FINE) {
+        float2 e, middle, tail;
+        normal_parts(z, e, middle, tail);
+        return make_float2(gelu_slope_of(z.x, e.x, middle.x, tail.x), gelu_slope_of(z.y, e.y, middle.y, tail.y));
     } else if constexpr (ACT == E3J_ACT_GELU) {   // Phi(z) + z phi(z)
         float2 e;
         const float2 beyond = __ffma2_rn(normal_tail(z, e), both(-1.f), both(0.5f));   // 1/2 - Phi(-|z|)
@@ -183,25 +227,26 @@ template <int ACT> __device__ __forceinline__ float2 slope(float2 z) {
         return __ffma2_rn(z, __fmul2_rn(e, both(0.39894228f)), Phi);
     } else return both(1.f);
 }
-template <int ACT, int N> __device__ __forceinline__ void activate_as(float2 (&v)[N]) {
+// (T: the type that the results are rounded to)
+template <int ACT, class T, int N> __device__ __forceinline__ void activate_as(float2 (&v)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = activation<ACT>(v[i]);
+    for (int i = 0; i < N; ++i) v[i] = activation<ACT, sizeof(T) == 4>(v[i]);
 }
 // g[i] *= slope(z[i])
-template <int ACT, int N> __device__ __forceinline__ void times_slope_as(float2 (&g)[N], const float2 (&z)[N]) {
+template <int ACT, class T, int N> __device__ __forceinline__ void times_slope_as(float2 (&g)[N], const float2 (&z)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) g[i] = __fmul2_rn(g[i], slope<ACT>(z[i]));
+    for (int i = 0; i < N; ++i) g[i] = __fmul2_rn(g[i], slope<ACT, sizeof(T) == 4>(z[i]));
 }
 // The same with the activation as a run-time value: one uniform branch for all elements.
-template <int N> __device__ __forceinline__ void activate(float2 (&v)[N], int act) {
-    if (act == E3J_ACT_SILU) activate_as<E3J_ACT_SILU>(v);
-    else if (act == E3J_ACT_TANH) activate_as<E3J_ACT_TANH>(v);
-    else if (act == E3J_ACT_GELU) activate_as<E3J_ACT_GELU>(v);
+template <class T, int N> __device__ __forceinline__ void activate(float2 (&v)[N], int act) {
+    if (act == E3J_ACT_SILU) activate_as<E3J_ACT_SILU, T>(v);
+    else if (act == E3J_ACT_TANH) activate_as<E3J_ACT_TANH, T>(v);
+    else if (act == E3J_ACT_GELU) activate_as<E3J_ACT_GELU, T>(v);
 }
-template <int N> __device__ __forceinline__ void times_slope(float2 (&g)[N], const float2 (&z)[N], int act) {
-    if (act == E3J_ACT_SILU) times_slope_as<E3J_ACT_SILU>(g, z);
-    else if (act == E3J_ACT_TANH) times_slope_as<E3J_ACT_TANH>(g, z);
-    else if (act == E3J_ACT_GELU) times_slope_as<E3J_ACT_GELU>(g, z);
+template <class T, int N> __device__ __forceinline__ void times_slope(float2 (&g)[N], const float2 (&z)[N], int act) {
+    if (act == E3J_ACT_SILU) times_slope_as<E3J_ACT_SILU, T>(g, z);
+    else if (act == E3J_ACT_TANH) times_slope_as<E3J_ACT_TANH, T>(g, z);
+    else if (act == E3J_ACT_GELU) times_slope_as<E3J_ACT_GELU, T>(g, z);
 }
 
 // launch_dependent with clusters of that many blocks.

@@ -210,9 +210,9 @@ __global__ void __launch_bounds__(kNormThreads, norm_blocks(V, EACH, RAGGED, BWD
             z[k] = __ffma2_rn(v[k], P::pair(w.r[k / H], k % H), P::pair(b.r[k / H], k % H));
         }
         if constexpr (!BWD) {
-            activate(z, a.act);
+            activate<T>(z, a.act);
         } else {
-            times_slope(g, z, a.act);
+            times_slope<T>(g, z, a.act);
             float2 mean_u = make_float2(0.f, 0.f), mean_uv = mean_u;
 #pragma unroll
             for (int k = 0; k < E2; ++k) {   // (g is zero in padding rows and outside the row)

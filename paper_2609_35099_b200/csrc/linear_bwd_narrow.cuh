@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) linear_bwd_narrow_kernel(co
                     if constexpr (kSlopes) {
                         const float4 b = *reinterpret_cast<const float4*>(bias + f);
                         const float2 z[2] = {__fadd2_rn(v.p[s][0], make_float2(b.x, b.y)), __fadd2_rn(v.p[s][1], make_float2(b.z, b.w))};
-                        times_slope_as<ACT>(g, z);
+                        times_slope_as<ACT, T>(g, z);
                     }
                     sum_b[0] = __fadd2_rn(sum_b[0], g[0]);
                     sum_b[1] = __fadd2_rn(sum_b[1], g[1]);

@@ -598,13 +598,13 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
                             }
                             if (row >= real) continue;
                             if constexpr (P == kForward) {
-                                activate_as<ACT>(z);
+                                activate_as<ACT, T>(z);
                                 if (meet) meets[c % kSlots][h][s].add_to(z);
                             }
                             if constexpr (P == kSlope) {
                                 float2 g[2] = {both(0.f), both(0.f)};
                                 meets[c % kSlots][h][s].add_to(g);
-                                times_slope_as<ACT>(g, z);
+                                times_slope_as<ACT, T>(g, z);
                                 store_quad<true>((float*)a.out + row * a.ld_gz + f, g, a.ld_gz - f);   // (whole vectors: ld_gz)
                             } else {
                                 store_quad<VO>((T*)a.out + row * width + f, z, width - f);
