@@ -123,22 +123,28 @@ def conv_vec(plan, graph: Graph, x, edge_vec, w) -> torch.Tensor:
     return _ConvVec.apply(plan, graph, x.contiguous(), edge_vec.contiguous(), w.contiguous())
 
 
+def _kept(ctx, n_real):
+    """A copy of a padded list's count of real rows for the backward: the next list may be prepared in the same buffer before it."""
+    return None if n_real is None or not any(ctx.needs_input_grad) else n_real.clone()
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, W, b, residual, act, n_real):
-        ctx.act, ctx.n_real = act, n_real
-        ctx.save_for_backward(x, W, b)
-        return e3j_linear_fwd(x, W, b, residual, act, n_real)
+        y = e3j_linear_fwd(x, W, b, residual, act, n_real)
+        ctx.act = act
+        ctx.save_for_backward(x, W, b, _kept(ctx, n_real))
+        return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad_y):
-        x, W, b = ctx.saved_tensors
+        x, W, b, n_real = ctx.saved_tensors
         grad_y, need = grad_y.contiguous(), ctx.needs_input_grad
-        gx, gW, gb = e3j_linear_bwd(x, W, b, grad_y, ctx.act, ctx.n_real, grad_x=need[0], grad_W=need[1], grad_b=need[2])
+        gx, gW, gb = e3j_linear_bwd(x, W, b, grad_y, ctx.act, n_real, grad_x=need[0], grad_W=need[1], grad_b=need[2])
         gr = grad_y if need[3] else None
-        if gr is not None and ctx.n_real is not None:   # padding rows of the result do not depend on anything
-            real = torch.arange(gr.shape[0], device=gr.device).unsqueeze(1) < ctx.n_real
+        if gr is not None and n_real is not None:   # padding rows of the result do not depend on anything
+            real = torch.arange(gr.shape[0], device=gr.device).unsqueeze(1) < n_real
             gr = torch.where(real, gr, torch.zeros_like(gr))
         return gx, gW, gb, gr, None, None
 
@@ -146,26 +152,27 @@ class _Linear(torch.autograd.Function):
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps, act, n_real):
-        ctx.eps, ctx.act, ctx.n_real = eps, act, n_real
-        ctx.save_for_backward(x, weight, bias)
-        return e3j_layer_norm_fwd(x, weight, bias, eps, act, n_real)
+        y = e3j_layer_norm_fwd(x, weight, bias, eps, act, n_real)
+        ctx.eps, ctx.act = eps, act
+        ctx.save_for_backward(x, weight, bias, _kept(ctx, n_real))
+        return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad_y):
-        x, weight, bias = ctx.saved_tensors
+        x, weight, bias, n_real = ctx.saved_tensors
         need = ctx.needs_input_grad
-        gx, gw, gb = e3j_layer_norm_bwd(x, weight, bias, grad_y.contiguous(), ctx.eps, ctx.act, ctx.n_real, grad_x=need[0],
+        gx, gw, gb = e3j_layer_norm_bwd(x, weight, bias, grad_y.contiguous(), ctx.eps, ctx.act, n_real, grad_x=need[0],
                                         grad_weight=need[1], grad_bias=need[2])
         return gx, gw, gb, None, None, None
 
 
 def linear(x, W, b=None, residual=None, act: int = E3J_ACT_NONE, n_real=None) -> torch.Tensor:
     """act(x W + b) + residual: x [rows, n_in], W [n_in, n_out] (float32 or bfloat16, first derivatives); saves x, W and b for the
-    backward, nothing else.  n_real as in e3j_linear_fwd."""
+    backward, nothing else.  n_real as in e3j_linear_fwd; its value at the time of the call counts for the backward too."""
     return _Linear.apply(x.contiguous(), W.contiguous(), _c(b), _c(residual), act, n_real)
 
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, act: int = E3J_ACT_NONE, n_real=None) -> torch.Tensor:
-    """Layer norm over the columns of x [rows, n] with an activation behind it (first derivatives); saves its inputs only."""
+    """Layer norm over the columns of x [rows, n] with an activation behind it (first derivatives); saves its inputs only.  n_real as in linear."""
     return _LayerNorm.apply(x.contiguous(), _c(weight), _c(bias), eps, act, n_real)

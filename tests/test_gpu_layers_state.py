@@ -1,0 +1,40 @@
+"""What the hidden layers rely on besides their inputs (GPU): the count of real rows until the backward, workspaces, what else is on the GPU."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2609_35099_b200 as e3j
+from paper_2609_35099_b200.autograd import layer_norm, linear
+
+pytestmark = pytest.mark.gpu
+SILU, GELU = e3j.E3J_ACT_SILU, e3j.E3J_ACT_GELU
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_count_of_real_rows_is_the_forward_s(dtype):
+    """A count that is rewritten for the next padded list before the backward of this one: by torch, and by a call of the library."""
+    rows, real = 500, 300
+    x, W, b, r, g, w = (torch.randn(*s, device="cuda").to(dtype).requires_grad_() for s in ((rows, 40), (40, 70), (70,), (rows, 70), (rows, 70), (70,)))
+    with torch.no_grad():
+        x[real:], r[real:], g[real:] = float("nan"), float("nan"), float("nan")
+
+    def by_torch(count):
+        count.fill_(450)
+
+    def by_the_library(count):   # (a row of four words; the count is the first of them)
+        words = torch.full((1, 4), 450, dtype=torch.int32, device="cuda").view(torch.float32)
+        e3j.e3j_rows_gather(count._base.view(torch.float32).view(1, 4), words, torch.zeros(1, dtype=torch.int32, device="cuda"))
+
+    def both(count, rewrite):
+        y = layer_norm(linear(x, W, b, r, SILU, count), w, act=GELU, n_real=count)
+        rewrite(count)
+        return torch.autograd.grad(y, (x, W, b, r, w), g)
+
+    count = lambda: torch.tensor([real] * 4, dtype=torch.int32, device="cuda")[:1]
+    want = both(count(), lambda c: None)
+    assert all(torch.isfinite(t.float()).all() for t in want)
+    for rewrite in (by_torch, by_the_library):
+        c = count()
+        got = both(c, rewrite)
+        assert c.item() == 450
+        assert all(torch.equal(p, q) for p, q in zip(got, want)), rewrite.__name__
