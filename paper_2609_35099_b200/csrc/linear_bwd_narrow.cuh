@@ -343,6 +343,9 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) linear_bwd_narrow_kernel(co
     umma::fence_before_sync();
     __syncthreads();
     umma::fence_after_sync();
+    // Tensor memory goes back before the cluster's blocks wait for one another: a block that has not got its own yet may be waiting for
+    // that of a block of another cluster, whose peer waits for this cluster's.
+    if (warp == kWorkWarps) umma::tmem_dealloc(tmem, 512);
     if (want_w && t < a.n_out) {
         float sum = 0.f;
         for (int q = 0; q < 4; ++q) sum += sums_of_warp[(t >> 4) * 4 + q][t & 15];
@@ -368,7 +371,6 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) linear_bwd_narrow_kernel(co
         }
         cluster.sync();   // (nobody leaves while others read)
     }
-    if (warp == kWorkWarps) umma::tmem_dealloc(tmem, 512);
 }
 
 }  // namespace layer

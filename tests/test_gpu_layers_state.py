@@ -38,3 +38,19 @@ def test_the_count_of_real_rows_is_the_forward_s(dtype):
         got = both(c, rewrite)
         assert c.item() == 450
         assert all(torch.equal(p, q) for p, q in zip(got, want)), rewrite.__name__
+
+
+def test_clusters_on_several_streams():
+    """Backward calls of few rows, one cluster each, on eight streams: more clusters at once than blocks of one that an SM could hold."""
+    shapes = [(1000, 64, 64), (900, 40, 64), (700, 64, 24), (1024, 8, 64)]
+    for dtype in (torch.bfloat16, torch.float32):
+        data = [[torch.randn(*s, device="cuda").to(dtype) for s in ((rows, n_in), (n_in, n_out), (n_out,), (rows, n_out))] for rows, n_in, n_out in shapes]
+        want = [e3j.e3j_linear_bwd(*t, SILU) for t in data]
+        torch.cuda.synchronize()
+        sides, got = [torch.cuda.Stream() for _ in range(8)], []
+        for k in range(200):
+            with torch.cuda.stream(sides[k % 8]):
+                got.append(e3j.e3j_linear_bwd(*data[k % 4], SILU))
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for k, t in enumerate(got) for p, q in zip(t, want[k % 4]))
+    assert e3j.e3j_linear_status() == 0
