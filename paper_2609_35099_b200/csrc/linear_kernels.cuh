@@ -304,10 +304,14 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
         abort_word = drain_word = 0;
         fast::mbar_fence_init();
     }
-    // Sums over rows that follow grad_x's product do not need it, and what came before that product is over when all of its blocks have
-    // got as far as their trigger: they run beside it, and only their end comes after its end.
+    // Sums over rows that follow grad_x's product do not need it: they run beside it, and their wait for it comes at their end (the second
+    // exception of fast::grid_dependency_wait).  They start when every block of that product has got as far as its trigger, behind its
+    // wait; so gz, x and the rest are written.  That these writes are seen is not that wait's promise to this kernel: a fence
+    // before the product's trigger and one here hand on what the product's threads may see.
     const bool beside = P == kGradW && a.beside;
-    if (!beside) fast::grid_dependency_wait();
+    if (beside) __threadfence();
+    else fast::grid_dependency_wait();
+    if (P == kGradX) __threadfence();
     fast::grid_dependency_trigger();
     // (a block that waits for another kernel holds no tensor memory, which a block of that kernel may be waiting for)
     if (warp == kIssuer) umma::tmem_alloc(&tmem_slot, L::kColumns);

@@ -54,3 +54,22 @@ def test_clusters_on_several_streams():
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for k, t in enumerate(got) for p, q in zip(t, want[k % 4]))
     assert e3j.e3j_linear_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,n_in,n_out,act", [(377, 104, 140, SILU), (377, 104, 140, 0), (1218, 96, 200, GELU), (3000, 33, 130, 0)])
+def test_sums_beside_grad_x_see_this_call_s_gradients(rows, n_in, n_out, act, dtype):
+    """Calls that follow one another with the same workspace and the same arrays, rewritten in between on the stream: the sums over rows,
+    which run beside grad_x's product, are those of the call without grad_x."""
+    x, W, g = (torch.empty(*s, device="cuda", dtype=dtype) for s in ((rows, n_in), (n_in, n_out), (rows, n_out)))
+    W.normal_()
+    room = torch.empty(max(1, e3j.e3j_linear_bwd_workspace_bytes(rows, n_in, n_out, act, int(dtype == torch.bfloat16))), dtype=torch.uint8, device="cuda")
+    xs, gs = [torch.randn_like(x) for _ in range(4)], [torch.randn_like(g) for _ in range(5)]
+    got, want = [], []
+    for k in range(60):
+        x.copy_(xs[k % 4])
+        g.copy_(gs[k % 5])
+        got.append(e3j.e3j_linear_bwd(x, W, None, g, act, workspace=room)[1:])
+    for k in range(20):
+        want.append(e3j.e3j_linear_bwd(xs[k % 4], W, None, gs[k % 5], act, grad_x=False)[1:])
+    assert all(torch.equal(p, q) for k in range(60) for p, q in zip(got[k], want[k % 20]))
