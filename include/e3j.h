@@ -334,7 +334,7 @@ int e3j_conv_radial_bwd(const e3j_plan* plan, int64_t n_nodes, int64_t n_edges, 
  * Backward: gz = grad_y act'(x W + b), formed again from x, W and b (the forward keeps nothing); grad_x = gz W^T, grad_W = x^T gz,
  * grad_b = sum over rows of gz; the residual's gradient is grad_y itself.  Any of grad_x, grad_W, grad_b may be NULL (not wanted).
  * Workspace: 256-byte aligned, e3j_linear_bwd_workspace_bytes() (0: none is needed, NULL will do); calls that overlap on the GPU must
- * not share it.
+ * not share it.  grad_x alone needs none without an activation or with both widths up to 64.
  * e3j_linear_status reads (and clears) the status word of these kernels on the current device into the HOST word *status: 0 =
  * fine, 1 = a bounded wait gave up and the outputs of some call are invalid.  Synchronises the device. */
 int e3j_linear_fwd(int dtype, int64_t rows, int n_in, int n_out, const void* x, const void* W, const void* b,

@@ -808,7 +808,9 @@ def e3j_linear_bwd(x, W, b, grad_y, act: int = E3J_ACT_NONE, n_real=None, grad_x
     dtype, (rows, n_in), n_out = x.dtype, x.shape, W.shape[-1]
     grad_x, grad_W = _wanted(grad_x, (rows, n_in), dtype, x), _wanted(grad_W, (n_in, n_out), dtype, x)
     grad_b = _wanted(grad_b, (n_out,), dtype, x)
-    room, size, workspace = _layer_workspace(_bytes("e3j_linear_bwd_workspace_bytes", code, rows, n_in, n_out, act), x, workspace, stream)
+    alone = grad_W is None and grad_b is None and (act == E3J_ACT_NONE or n_in <= 64 and n_out <= 64)   # needs no workspace
+    nbytes = 0 if alone else _bytes("e3j_linear_bwd_workspace_bytes", code, rows, n_in, n_out, act)
+    room, size, workspace = _layer_workspace(nbytes, x, workspace, stream)
     _run("e3j_linear_bwd", code, rows, n_in, n_out, _dev_ptr(x, dtype, None, "x"), _dev_ptr(W, dtype, (n_in, n_out), "W"),
          _dev_ptr(b, dtype, (n_out,), "b"), _dev_ptr(grad_y, dtype, (rows, n_out), "grad_y"), act,
          _dev_ptr(n_real, _torch_module.int32, (1,), "n_real"), _dev_ptr(grad_x, dtype, (rows, n_in), "grad_x"),
@@ -856,7 +858,8 @@ def e3j_layer_norm_bwd(x, weight, bias, grad_y, eps: float = 1e-5, act: int = E3
     dtype, (rows, n) = x.dtype, x.shape
     grad_x, grad_weight = _wanted(grad_x, (rows, n), dtype, x), _wanted(grad_weight, (n,), dtype, x)
     grad_bias = _wanted(grad_bias, (n,), dtype, x)
-    room, size, workspace = _layer_workspace(_bytes("e3j_layer_norm_bwd_workspace_bytes", code, rows, n), x, workspace, stream)
+    nbytes = 0 if grad_weight is None and grad_bias is None else _bytes("e3j_layer_norm_bwd_workspace_bytes", code, rows, n)
+    room, size, workspace = _layer_workspace(nbytes, x, workspace, stream)
     _run_real("e3j_layer_norm_bwd", 7, float(eps), code, rows, n, _dev_ptr(x, dtype, None, "x"), _dev_ptr(weight, dtype, (n,), "weight"),
               _dev_ptr(bias, dtype, (n,), "bias"), _dev_ptr(grad_y, dtype, (rows, n), "grad_y"), act,
               _dev_ptr(n_real, _torch_module.int32, (1,), "n_real"), _dev_ptr(grad_x, dtype, (rows, n), "grad_x"),

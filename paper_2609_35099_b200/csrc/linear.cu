@@ -111,7 +111,8 @@ int e3j_linear_bwd(int dtype, int64_t rows, int n_in, int n_out, const void* x, 
     if (!x || !W || !grad_y) return E3J_ERR_INVALID_ARG;
     if (!grad_x && !grad_W && !grad_b) return E3J_OK;
     const BwdLayout L = bwd_layout(dtype, rows, n_in, n_out, act);
-    if (L.total > 0 && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < L.total)) return E3J_ERR_WORKSPACE;
+    const size_t need = grad_W || grad_b ? L.total : L.shares;   // (grad_x alone: gz, if that is in memory)
+    if (need > 0 && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need)) return E3J_ERR_WORKSPACE;
     LinArgs a{};
     a.rows = rows; a.n_in = n_in; a.n_out = n_out; a.n_real = n_real;
     if (int rc = status_word(&a.status)) return rc;

@@ -129,19 +129,19 @@ template <class T, class G> int gradients(LinArgs a, const BwdLayout& L, void* g
     return sum_shares<T>(L.ranges, (int64_t)a.n_in * a.n_out, a.n_out, a.shares, (T*)grad_W, (T*)grad_b, st);
 }
 
-template <class T, int ACT, bool VEC> int narrow_kernel(LinArgs& a, int blocks, cudaStream_t st) {
+template <class T, int ACT, bool VEC> int narrow_kernel(LinArgs& a, int blocks, bool direct, cudaStream_t st) {
     using S = NarrowLayout<T, ACT>;
     constexpr auto kernel = linear_bwd_narrow_kernel<T, ACT, VEC>;
     static std::atomic<uint64_t> allowed{0};
     if (int rc = allow_smem(kernel, S::smem, allowed)) return rc;
-    return launch_cluster(kernel, blocks, a.shares ? 1 : blocks, kNarrowThreads, S::smem, st, a);
+    return launch_cluster(kernel, blocks, direct ? blocks : 1, kNarrowThreads, S::smem, st, a);
 }
 template <class T, int ACT> int narrow_bwd(LinArgs& a, const BwdLayout& L, void* grad_W, void* grad_b, cudaStream_t st) {
     const bool vector = whole(a.x, a.n_in, sizeof(T)) && whole(a.W, a.n_out, sizeof(T)) && whole(a.grad_y, a.n_out, sizeof(T)) &&
                         whole(a.out, a.n_in, sizeof(T));
     a.grad_W = grad_W;
     a.grad_b = grad_b;
-    if (int rc = vector ? narrow_kernel<T, ACT, true>(a, L.ranges, st) : narrow_kernel<T, ACT, false>(a, L.ranges, st)) return rc;
+    if (int rc = vector ? narrow_kernel<T, ACT, true>(a, L.ranges, L.direct, st) : narrow_kernel<T, ACT, false>(a, L.ranges, L.direct, st)) return rc;
     if (L.direct || (!grad_W && !grad_b)) return E3J_OK;
     return sum_shares<T>(L.ranges * NarrowLayout<T, ACT>::parts, (int64_t)a.n_in * a.n_out, a.n_out, a.shares, (T*)grad_W, (T*)grad_b, st);
 }

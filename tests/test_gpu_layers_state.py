@@ -73,3 +73,34 @@ def test_sums_beside_grad_x_see_this_call_s_gradients(rows, n_in, n_out, act, dt
     for k in range(20):
         want.append(e3j.e3j_linear_bwd(xs[k % 4], W, None, gs[k % 5], act, grad_x=False)[1:])
     assert all(torch.equal(p, q) for k in range(60) for p, q in zip(got[k], want[k % 20]))
+
+
+def bwd_without_room(x, W, g, act, gx, dtype):
+    """The C entry point with no workspace, for grad_x alone."""
+    rows, n_in = x.shape
+    return e3j._load().e3j_linear_bwd(dtype, rows, n_in, W.shape[1], x.data_ptr(), W.data_ptr(), None, g.data_ptr(), act, None, gx.data_ptr(),
+                                      None, None, None, 0, torch.cuda.current_stream().cuda_stream)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,n_in,n_out,act", [(5000, 64, 64, SILU), (5000, 30, 17, 0), (200, 64, 64, GELU), (5000, 100, 70, 0), (40000, 64, 64, GELU)])
+def test_grad_x_alone_needs_no_room_for_shares(rows, n_in, n_out, act, dtype):
+    x, W, g = (torch.randn(*s, device="cuda").to(dtype) for s in ((rows, n_in), (n_in, n_out), (rows, n_out)))
+    want = e3j.e3j_linear_bwd(x, W, None, g, act)[0]
+    gx = torch.full_like(x, float("nan"))
+    assert bwd_without_room(x, W, g, act, gx, int(dtype == torch.bfloat16)) == 0
+    assert torch.equal(gx, want)
+    gx.fill_(float("nan"))
+    before = torch.cuda.memory_stats()["allocation.all.allocated"]
+    e3j.e3j_linear_bwd(x, W, None, g, act, grad_x=gx, grad_W=False, grad_b=False)
+    e3j.e3j_layer_norm_bwd(x, None, None, x, grad_x=gx, grad_weight=False, grad_bias=False)
+    assert torch.cuda.memory_stats()["allocation.all.allocated"] == before
+    e3j.e3j_linear_bwd(x, W, None, g, act, grad_x=gx, grad_W=False, grad_b=False)
+    assert torch.equal(gx, want)
+
+
+def test_with_an_activation_beyond_64_columns_room_for_gz_is_still_asked_for():
+    x, W, g = torch.randn(5000, 100, device="cuda"), torch.randn(100, 70, device="cuda"), torch.randn(5000, 70, device="cuda")
+    gx = torch.empty_like(x)
+    assert bwd_without_room(x, W, g, SILU, gx, 0) == e3j.E3J_ERR_WORKSPACE
+    assert torch.equal(e3j.e3j_linear_bwd(x, W, None, g, SILU, grad_W=False, grad_b=False)[0], e3j.e3j_linear_bwd(x, W, None, g, SILU)[0])
