@@ -17,8 +17,11 @@
 // Accumulators.  The tensor cores add with truncation, so long chains drift (see radial_gemm.cuh).  Of float32 operands the
 // hi hi products go to one accumulator and the five smaller ones to another (B's hi and mid lie behind one another, so the first
 // two are one instruction of twice the width), and a chain ends after kChain of the contraction, 16 additions of hi hi: the readers
-// add the chains in registers, rounding.  Products over up to kLongest columns are one chain of 32 at most (2-norm of the error,
-// normal values: 1.1e-7 with 64, 5e-7 with 512; 4096 would be 4.6e-6).
+// add the chains, rounding: in products over up to kLongest columns when they read a tile, whose two chains are in accumulator
+// sets of their own (PAIR); beyond that, and over rows, in registers (LONG).
+// An instruction of 16 products loses 3 half steps of the sum on average (measured: each product is cut off at a quarter of a half
+// step of the sum, and the sum at a whole step).  2-norm of the error, normal values: 1.1e-7 with 64 columns, 2.8e-7 with 256, 512
+// (5.3e-7 in one chain) and 4096 (4.6e-6).
 //
 // Order of a tile's columns.  A quad of lanes reads tensor memory in pieces of 8 columns, two a lane (tcgen05.ld 16x256b).  Columns
 // of a 16-column group are dealt out so that the two pieces of a lane are four consecutive features: rows leave in 64-byte (float32) or
@@ -44,8 +47,8 @@ constexpr int lin_threads(int size) { return read_warps(size) * 32 + kRoleThread
 constexpr int kMostStages = 6;
 constexpr int kTileRows = 128;      // accumulator lanes
 constexpr int kChunk = 64;          // contraction elements a chunk
-constexpr int kChain = 256;         // contraction elements a chain is long (sums over rows; LONG products)
-constexpr int kLongest = 512;       // ... of other products
+constexpr int kChain = 256;         // contraction elements a chain is long (float32)
+constexpr int kLongest = 2 * kChain;   // ... up to which the two accumulator sets hold a tile's chains
 
 // ---------------------------------------------------------------- operands
 // Four consecutive elements, `left` of which are there, as they lie in memory.
@@ -259,7 +262,10 @@ template <class T, class G> struct Types<kGradW, T, G> {
 };
 
 // VA: A's rows start on 16 bytes; VO: those of B, of the results and of what they meet do.
-template <Product P, class T, class G, int NT, bool VA, bool VO> struct LinTile {
+// CHAINS of float32 products that a tile's contraction is cut into: kOne; kPair, one in either of two accumulator sets (more than kChain
+// columns); kMany, added in registers (more than kLongest).
+enum Chains { kOne, kPair, kMany };
+template <Product P, class T, class G, int NT, bool VA, bool VO, Chains CHAINS> struct LinTile {
     using Ty = Types<P, T, G>;
     static constexpr bool kRowSum = P == kGradW;    // contraction over rows: both operands MN-major
     // Sums over rows of float32 take 32 rows at a time: with 64 the loaders' registers do not hold both operands of a chunk, and what
@@ -268,25 +274,27 @@ template <Product P, class T, class G, int NT, bool VA, bool VO> struct LinTile 
     using OpA = Operand<typename Ty::A, Ty::a_terms, kRowSum ? kRows : kTileRows, kRowSum ? kTileRows : kChunk, false, VA>;
     using OpB = Operand<typename Ty::B, Ty::b_terms, P == kGradX ? NT : kRows, P == kGradX ? kChunk : NT, P != kGradX, VO>;
     static constexpr bool kA_mn = kRowSum, kB_mn = P != kGradX;
-    static constexpr int kSets = Ty::a_terms == 3 ? 2 : 1;     // accumulators of a tile
-    static constexpr int kColumns = 2 * kSets * NT;            // tensor memory: two tiles
+    static constexpr int kSets = Ty::a_terms == 3 ? 2 : 1;     // accumulators of a chain
+    static constexpr int kUnits = CHAINS == kPair && NT == 64 ? 4 : 2;   // chains in tensor memory: two tiles' (kPair with NT 128: one's)
+    static constexpr int kColumns = kUnits * kSets * NT;
     static constexpr bool kAsyncA = VA && sizeof(typename Ty::A) == 2;   // A by cp.async ...
     static constexpr bool kBoxes = kAsyncA && !kRowSum;                  // ... or by tiled bulk copies (LinArgs::boxes)
     static size_t smem_bytes(int stages, int b_slots) { return 1024 + (size_t)stages * OpA::kBytes + (size_t)b_slots * OpB::kBytes; }
 };
 
-// LONG: the contraction is cut into chains (float32 products over more than kLongest columns).
-template <Product P, class T, class G, int NT, int ACT, bool VA, bool VO, bool LONG>
+template <Product P, class T, class G, int NT, int ACT, bool VA, bool VO, Chains CHAINS>
 __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const __grid_constant__ LinArgs a) {
-    using L = LinTile<P, T, G, NT, VA, VO>;
+    using L = LinTile<P, T, G, NT, VA, VO, CHAINS>;
     using TA = typename L::Ty::A;
     using TB = typename L::Ty::B;
     using OpA = typename L::OpA;
     using OpB = typename L::OpB;
     constexpr int kTermsA = L::Ty::a_terms, kTermsB = L::Ty::b_terms;
+    constexpr bool LONG = CHAINS == kMany, PAIR = CHAINS == kPair;
+    static_assert(!PAIR || (P != kGradW && L::kSets == 2), "two accumulators a chain, a chain in either set");
     constexpr int kChunkRows = L::kRows, kGroupChunks = kChain / L::kRows;   // chunks a chain
     extern __shared__ unsigned char raw_smem[];
-    __shared__ uint64_t full[kMostStages], empty[kMostStages], tile_full[2], tile_empty[2], drain;
+    __shared__ uint64_t full[kMostStages], empty[kMostStages], tile_full[4], tile_empty[4], drain;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word, drain_word;
     __shared__ float column_sums[P == kGradW ? OpB::kRows * NT : 1];   // (1024)
@@ -299,7 +307,7 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kMostStages; ++i) { fast::mbar_init(&full[i], L::kBoxes && a.boxes ? 1 : kLoaders); fast::mbar_init(&empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { fast::mbar_init(&tile_full[i], 1); fast::mbar_init(&tile_empty[i], kReaders); }
+        for (int i = 0; i < L::kUnits; ++i) { fast::mbar_init(&tile_full[i], 1); fast::mbar_init(&tile_empty[i], kReaders); }
         fast::mbar_init(&drain, 1);
         abort_word = drain_word = 0;
         fast::mbar_fence_init();
@@ -322,9 +330,9 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
             bias[threadIdx.x] = a.b && n0 + (int)threadIdx.x < a.n_out ? to_float(((const T*)a.b)[n0 + threadIdx.x]) : 0.f;
     const int64_t real = real_rows(a.rows, a.n_real);
 
-    // ---- what this block does: units (a tile, or for kGradW and LONG a chain of one tile) of up to `chunks` chunks
+    // ---- what this block does: units (a tile, or for kGradW, LONG and PAIR a chain of one tile) of up to `chunks` chunks
     int units, chunks, m0 = 0;
-    int chains = 1;                            // LONG: units of a tile
+    int chains = 1;                            // LONG: units of a tile (PAIR: two)
     int64_t unit0 = 0, unit_step = 1;          // row tiles of this block
     int64_t chunk_begin = 0, chunk_end = 0;    // kGradW: chunks of rows of this block
     if constexpr (P == kGradW) {
@@ -345,13 +353,14 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
             chains = (chunks + kGroupChunks - 1) / kGroupChunks;
             units *= chains;
         }
+        if constexpr (PAIR) units *= 2;
     }
     // of a unit: its tile's first row, its first chunk
-    auto row_of = [&](int unit) { return (unit0 + (LONG ? unit / chains : unit) * unit_step) * kTileRows; };
-    auto first_chunk = [&](int unit) { return LONG ? unit % chains * kGroupChunks : 0; };
+    auto row_of = [&](int unit) { return (unit0 + (LONG ? unit / chains : PAIR ? unit >> 1 : unit) * unit_step) * kTileRows; };
+    auto first_chunk = [&](int unit) { return LONG ? unit % chains * kGroupChunks : PAIR ? (unit & 1) * kGroupChunks : 0; };
     auto chunks_of = [&](int unit) {
         if constexpr (P == kGradW) return (int)min((int64_t)kGroupChunks, chunk_end - chunk_begin - (int64_t)unit * kGroupChunks);
-        else if constexpr (LONG) return min(kGroupChunks, chunks - first_chunk(unit));
+        else if constexpr (LONG || PAIR) return min(kGroupChunks, chunks - first_chunk(unit));
         else return chunks;
     };
     unsigned char* const b_area = smem + (size_t)a.stages * OpA::kBytes;
@@ -496,8 +505,8 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
             bool ok = true;
             for (int unit = 0; ok && unit < units; ++unit) {
                 const int n_chunks = chunks_of(unit);
-                const int set = unit & 1;
-                if (unit >= 2 && !(ok = fast::mbar_wait(&tile_empty[set], ((unit >> 1) - 1) & 1, abort_flag, a.status))) break;
+                const int set = unit % L::kUnits;
+                if (unit >= L::kUnits && !(ok = fast::mbar_wait(&tile_empty[set], (unit / L::kUnits - 1) & 1, abort_flag, a.status))) break;
                 const uint32_t d = tmem + (uint32_t)(set * L::kSets * NT);
                 for (int chunk = 0; chunk < n_chunks; ++chunk) {
                     if (!(ok = fast::mbar_wait(&full[stage], turn & 1, abort_flag, a.status))) break;
@@ -546,8 +555,8 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
         const int width = P == kGradX ? a.n_in : a.n_out;
         const int f0 = n0 + first + 4 * (lane & 3);               // first of this lane's four features in the first group
         const T* const meet = (const T*)(P == kForward ? a.residual : a.grad_y);
-        for (int unit = 0; unit < units; ++unit) {
-            const int set = unit & 1;
+        for (int unit = 0; unit < units; unit += PAIR ? 2 : 1) {
+            const int set = unit % L::kUnits;
             const int64_t row0 = row_of(unit) + quarter * 32 + lane / 4;
             const bool whole = !LONG || (unit + 1) % chains == 0;   // this unit finishes the tile
             auto fetch = [&](int c) {
@@ -560,7 +569,9 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
             if (kMeets && meet && whole)
 #pragma unroll
                 for (int c = 0; c < kSlots; ++c) fetch(c);
-            if (!fast::mbar_wait(&tile_full[set], (unit >> 1) & 1, abort_flag, a.status)) break;
+            const int phase = unit / L::kUnits & 1;
+            if (!fast::mbar_wait(&tile_full[set], phase, abort_flag, a.status)) break;
+            if (PAIR && !fast::mbar_wait(&tile_full[set + 1], phase, abort_flag, a.status)) break;
             umma::fence_after_sync();
 #pragma unroll
             for (int c = 0; c < kGroups; ++c) {
@@ -578,6 +589,13 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
                         tmem_ld_quads(taddr + NT, u);
                         umma::tmem_ld_wait();
                         add_quads(v, u);
+                        if constexpr (PAIR)
+#pragma unroll
+                            for (int k = 2; k < 4; ++k) {
+                                tmem_ld_quads(taddr + k * NT, u);
+                                umma::tmem_ld_wait();
+                                add_quads(v, u);
+                            }
                     } else {
                         umma::tmem_ld_wait();
                     }
@@ -620,7 +638,10 @@ __global__ void __launch_bounds__(lin_threads(sizeof(T)), 1) linear_kernel(const
             }
             umma::fence_before_sync();
             __syncwarp();
-            if (lane == 0) fast::mbar_arrive(&tile_empty[set]);
+            if (lane == 0) {
+                fast::mbar_arrive(&tile_empty[set]);
+                if (PAIR) fast::mbar_arrive(&tile_empty[set + 1]);
+            }
         }
         if constexpr (P == kGradW) {
             const int range = blockIdx.x / (a.n_tiles * a.m_tiles);

@@ -35,10 +35,10 @@ inline bool box_map(CUtensorMap* map, const void* base, int64_t rows, int column
                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <Product P, class T, class G, int NT, int ACT, bool VA, bool VO, bool LONG = false>
+template <Product P, class T, class G, int NT, int ACT, bool VA, bool VO, Chains CHAINS = kOne>
 struct Launch {
-    using L = LinTile<P, T, G, NT, VA, VO>;
-    static constexpr auto kernel = linear_kernel<P, T, G, NT, ACT, VA, VO, LONG>;
+    using L = LinTile<P, T, G, NT, VA, VO, CHAINS>;
+    static constexpr auto kernel = linear_kernel<P, T, G, NT, ACT, VA, VO, CHAINS>;
     static constexpr size_t kStatic = (P == kGradW ? 1024 : NT) * sizeof(float) + 512;
     // Operand stages, and whether all of B's chunks stay in shared memory (with two stages at least).
     static int shape(LinArgs& a, int chunks, size_t& smem) {
@@ -55,10 +55,10 @@ struct Launch {
     static int run(LinArgs& a, cudaStream_t st) {
         static std::atomic<uint64_t> allowed{0};
         if (int rc = allow_smem(kernel, kSmemOfBlock - kStatic, allowed)) return rc;
-        const int columns = P == kGradX ? a.n_in : a.n_out;
+        const int columns = P == kGradX ? a.n_in : a.n_out, contraction = P == kGradX ? a.n_out : a.n_in;
         a.n_tiles = (columns + NT - 1) / NT;
         size_t smem = 0;
-        if (int rc = shape(a, ((P == kGradX ? a.n_out : a.n_in) + kChunk - 1) / kChunk, smem)) return rc;
+        if (int rc = shape(a, (contraction + kChunk - 1) / kChunk, smem)) return rc;
         int64_t grid;
         if (P == kGradW) {
             grid = (int64_t)a.n_tiles * a.m_tiles * a.ranges;
@@ -78,6 +78,12 @@ struct Launch {
 
 // Which rows start on 16 bytes: those of A; all others (B's, and but for kGradW those of the results and of what they meet).
 struct Aligned { bool a, others; };
+template <Product P, class T, class G, int ACT, Chains CHAINS> int product_of(LinArgs& x, Aligned v, bool narrow, cudaStream_t st) {
+    if (v.a && v.others) return narrow ? Launch<P, T, G, 64, ACT, true, true, CHAINS>::run(x, st) : Launch<P, T, G, 128, ACT, true, true, CHAINS>::run(x, st);
+    if (v.a) return narrow ? Launch<P, T, G, 64, ACT, true, false, CHAINS>::run(x, st) : Launch<P, T, G, 128, ACT, true, false, CHAINS>::run(x, st);
+    if (v.others) return narrow ? Launch<P, T, G, 64, ACT, false, true, CHAINS>::run(x, st) : Launch<P, T, G, 128, ACT, false, true, CHAINS>::run(x, st);
+    return narrow ? Launch<P, T, G, 64, ACT, false, false, CHAINS>::run(x, st) : Launch<P, T, G, 128, ACT, false, false, CHAINS>::run(x, st);
+}
 template <Product P, class T, class G, int ACT = E3J_ACT_NONE> int product(LinArgs& x, Aligned v, cudaStream_t st) {
     const int columns = P == kGradX ? x.n_in : x.n_out;
     // Tiles of 64 columns instead of 128: where there are no more columns; with float32 where they leave fewer columns of the tiles empty
@@ -86,13 +92,14 @@ template <Product P, class T, class G, int ACT = E3J_ACT_NONE> int product(LinAr
     // forward: 14.9 us with tiles of 128, 11.6 so).
     const bool fewer = P != kGradW && sizeof(T) == 4 && (columns - 1) % 128 < 64;
     const bool narrow = columns <= 64 || fewer || (P != kGradW && (x.rows + kTileRows - 1) / kTileRows * ((columns + 63) / 64) <= sm_count());
-    if constexpr (P != kGradW && sizeof(T) == 4)   // (tiles of 64: the sums of the chains are registers)
-        if ((P == kGradX ? x.n_out : x.n_in) > kLongest)
-            return v.a && v.others ? Launch<P, T, G, 64, ACT, true, true, true>::run(x, st) : Launch<P, T, G, 64, ACT, false, false, true>::run(x, st);
-    if (v.a && v.others) return narrow ? Launch<P, T, G, 64, ACT, true, true>::run(x, st) : Launch<P, T, G, 128, ACT, true, true>::run(x, st);
-    if (v.a) return narrow ? Launch<P, T, G, 64, ACT, true, false>::run(x, st) : Launch<P, T, G, 128, ACT, true, false>::run(x, st);
-    if (v.others) return narrow ? Launch<P, T, G, 64, ACT, false, true>::run(x, st) : Launch<P, T, G, 128, ACT, false, true>::run(x, st);
-    return narrow ? Launch<P, T, G, 64, ACT, false, false>::run(x, st) : Launch<P, T, G, 128, ACT, false, false>::run(x, st);
+    if constexpr (P != kGradW && sizeof(T) == 4) {
+        const int contraction = P == kGradX ? x.n_out : x.n_in;
+        if (contraction > kLongest)   // (tiles of 64: the sums of the chains are registers)
+            return v.a && v.others ? Launch<P, T, G, 64, ACT, true, true, kMany>::run(x, st) : Launch<P, T, G, 64, ACT, false, false, kMany>::run(x, st);
+        // (as kMany 40 000 x 512 -> 256 takes 125 us; in one chain, half as exact, 83; so 91)
+        if (contraction > kChain) return product_of<P, T, G, ACT, kPair>(x, v, narrow, st);
+    }
+    return product_of<P, T, G, ACT, kOne>(x, v, narrow, st);
 }
 template <Product P, class T, class G> int product_act(LinArgs& a, int act, Aligned v, cudaStream_t st) {
     if (act == E3J_ACT_SILU) return product<P, T, G, E3J_ACT_SILU>(a, v, st);
