@@ -323,8 +323,10 @@ NormShape norm_shape(int64_t rows, int n, int size, bool bwd, bool aligned) {
     const int64_t per_turn = kNormThreads / s.lanes;
     const int64_t resident = (int64_t)sm_count() * norm_blocks(s.vector ? v : 1, s.each, s.ragged, bwd);
     s.blocks = (int)std::min<int64_t>((rows + per_turn - 1) / per_turn, resident);
-    // Few rows, backward: one cluster, whose blocks take up to kClusterTurns turns, and no second kernel for the sums (1201 rows of
-    // 64: 14.3 us with it, 9.5 without, both bound by the host).
+    // Few rows, backward: one cluster, whose blocks take up to kClusterTurns turns, and no second kernel for the sums.  What counts is the host,
+    // which calls of this size wait for: 9.1 us a call where two kernels are 13.1, as long as the cluster is not slower than that (on
+    // the device, cluster and two kernels: 1536 x 64 float32, 6 turns, 6.5 and 4.4 us; 384 x 512 bfloat16, 6 turns, 11.8 and 6.7; 192 x 385
+    // 13.9 and 6.6; with 12 turns 760 x 512 18.6 and 6.9).
     s.direct = bwd && rows <= kClusterBlocks * kClusterTurns * per_turn;
     if (s.direct) s.blocks = std::min(s.blocks, kClusterBlocks);
     const int step = (int)std::max<int64_t>(v / per_turn, 1);   // (ragged rows: the stride is a multiple of v rows)
