@@ -86,14 +86,22 @@ template <Product P, class T, class G, int ACT, Chains CHAINS> int product_of(Li
 }
 template <Product P, class T, class G, int ACT = E3J_ACT_NONE> int product(LinArgs& x, Aligned v, cudaStream_t st) {
     const int columns = P == kGradX ? x.n_in : x.n_out;
-    // Tiles of 64 columns instead of 128: where there are no more columns; with float32 where they leave fewer columns of the tiles empty
-    // (41 003 rows, 97 -> 161: x W and the slope 48 us with tiles of 128, 38 so; 60 000 x 128 -> 128 21.3 and 26.3, so not elsewhere;
-    // sums over rows, 38 and 44, not either); and where every one of them has an SM of its own (1218 rows of 336 -> 328 float32
-    // forward: 14.9 us with tiles of 128, 11.6 so).
-    const bool fewer = P != kGradW && sizeof(T) == 4 && (columns - 1) % 128 < 64;
+    // Tiles of 64 columns instead of 128: where there are no more columns; where every one of them has an SM of its own (1218 rows of 336
+    // -> 328 float32 forward: 14.9 us with tiles of 128, 11.6 so); and with float32, not in sums over rows (38 and 44 us), where they
+    // leave fewer columns of the tiles empty and
+    // - the rows that they meet are off 16 bytes, so that loaders and readers pay by the column (60 000 rows forward, with 128 and 64: 33 -> 161
+    //   46.9 and 36.0, 97 -> 161 60.8 and 49.3, 33 -> 257 59.8 and 51.3, 33 -> 513 96.7 and 88.4, 97 -> 290 86.6 and 80.1; grad_x 161 <- 97
+    //   61.2 and 54.0), or
+    // - two of these hold, not in grad_x: readers have a residual or grad_y to fetch, W is one chunk, there are no more than 192 columns
+    //   (all three 27.9 and 27.7; fetching, 128 -> 160 39.7 and 36.3, 256 -> 160 63.8 and 61.7, 64 -> 288 51.0 and 47.9; without, 32 -> 160 22.4
+    //   and 18.8, 64 -> 192 23.8 and 22.0).
+    // Not with one or none (fetching, 128 -> 288 54.7 and 57.3, 256 -> 288 87.6 and 100.0; without, 96 -> 160 27.4 and 30.5, 64 -> 288 32.3 and
+    // 35.1, 128 -> 288 40.6 and 55.6; grad_x 192 <- 64 20.1 and 20.5, 288 <- 128 40.3 and 53.1).
+    const int contraction = P == kGradX ? x.n_out : x.n_in;
+    const int reasons = (P == kSlope || (P == kForward && x.residual)) + (contraction <= kChunk) + (columns <= 192);
+    const bool fewer = P != kGradW && sizeof(T) == 4 && (columns - 1) % 128 < 64 && (!v.others || (P != kGradX && reasons >= 2));
     const bool narrow = columns <= 64 || fewer || (P != kGradW && (x.rows + kTileRows - 1) / kTileRows * ((columns + 63) / 64) <= sm_count());
     if constexpr (P != kGradW && sizeof(T) == 4) {
-        const int contraction = P == kGradX ? x.n_out : x.n_in;
         if (contraction > kLongest)   // (tiles of 64: the sums of the chains are registers)
             return v.a && v.others ? Launch<P, T, G, 64, ACT, true, true, kMany>::run(x, st) : Launch<P, T, G, 64, ACT, false, false, kMany>::run(x, st);
         // (as kMany 40 000 x 512 -> 256 takes 125 us; in one chain, half as exact, 83; so 91)

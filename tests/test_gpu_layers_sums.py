@@ -27,3 +27,16 @@ def test_contractions_of_every_length_are_cut_into_chains(k):
     grad_x = e3j.e3j_linear_bwd(x[:, :200].contiguous(), W.t().contiguous(), None, x, grad_W=False, grad_b=False)[0]
     for got in (forward, grad_x):
         assert abs(((got.double() - want) / want).mean().item()) <= 52 * U
+
+
+@pytest.mark.parametrize("n_in", [32, 64, 96, 300, 520])
+@pytest.mark.parametrize("n_out", [64, 129, 160, 192, 257, 288])
+def test_a_tile_s_width_does_not_change_bits(n_in, n_out):
+    """Tiles are 64 or 128 columns wide by rules on sizes, rows and what the results meet; a result's sums are the same in both."""
+    x, W, b = torch.randn(20000, n_in, device="cuda"), torch.randn(n_in, n_out, device="cuda"), torch.randn(n_out, device="cuda")
+    y = e3j.e3j_linear_fwd(x, W, b)
+    assert torch.equal(y, e3j.e3j_linear_fwd(x, W, b, torch.zeros_like(y)))
+    assert torch.equal(y[:100], e3j.e3j_linear_fwd(x[:100], W, b))
+    if n_out % 64 == 0:
+        room = torch.empty(y.numel() + 1, device="cuda")[1:].view(y.shape)   # (rows off 16 bytes)
+        assert torch.equal(y, e3j.e3j_linear_fwd(x, W, b, out=room))
