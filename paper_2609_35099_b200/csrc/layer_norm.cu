@@ -9,7 +9,8 @@
 // and variance (about the mean: two sums one after the other, no cancellation) cost shuffles, not traffic, and the backward
 // forms them again from the x that it has to read anyway instead of having the forward write them.  A lane has 8 elements of a
 // row: with fewer, what a row costs once (the sums' shuffles, the root) bounds narrow rows.  So a row of 64 is shared by 8 lanes, four
-// rows a warp; from 256 columns on it is 16 elements and whole warps, up to eight of them a row.  Arithmetic on pairs
+// rows a warp; beyond 256 columns it is whole warps, up to eight of them a row, and 16 elements where the registers hold them
+// (sixteen_elements), beyond 2048 columns anyway.  Arithmetic on pairs
 // (packed float32 instructions), since with 2-byte elements the instructions, not the memory, come first.
 //
 // The parameters' gradients are sums over all rows: every lane adds up its columns over the rows it meets, the warps of a
@@ -66,6 +67,8 @@ template <int LANES> struct RowSum {
     __device__ __forceinline__ float operator()(float v) { return (*this)(make_float2(v, 0.f)).x; }
 };
 
+// Whether lanes have 16 elements of rows beyond 256 columns, not of those beyond 2048 alone: fewer lanes to sum over.
+__host__ __device__ constexpr bool sixteen_elements(int size, bool vector, bool ragged, bool bwd) { return !bwd || (size == 2 && vector && !ragged); }
 // Blocks an SM: as many as the registers allow (nearly) without spilling.
 __host__ __device__ constexpr int norm_blocks(int v, int each, bool ragged, bool bwd) {
     return v == 1 ? (each == 8 && !bwd ? 2 : 1)
@@ -313,10 +316,8 @@ NormShape norm_shape(int64_t rows, int n, int size, bool bwd, bool aligned) {
     const int v = 16 / size;
     s.ragged = aligned && n % v != 0 && n > 32 && n + v - 1 <= 16 * kNormThreads;
     s.vector = aligned && (n % v == 0 || s.ragged);
-    // Elements a lane: 8, or 16 in rows of more than 256 (fewer lanes to sum over) unless the backward's registers would not
-    // hold them, and whenever 8 are not enough.
     const int width = n + (s.ragged ? v - 1 : 0);
-    s.each = width > 8 * kNormThreads || (width > 256 && (!bwd || (size == 2 && s.vector && !s.ragged))) ? 16 : 8;
+    s.each = width > 8 * kNormThreads || (width > 256 && sixteen_elements(size, s.vector, s.ragged, bwd)) ? 16 : 8;
     s.lanes = 1;
     while (s.lanes * s.each < width) s.lanes *= 2;
     if (s.each == 16) s.lanes = std::max(s.lanes, 32);
@@ -339,16 +340,19 @@ template <class T, int V, int EACH, int LANES, bool RAGGED, bool BWD> int launch
                           BWD ? sizeof(float) * 2 * (size_t)a.n * (LANES ? kNormWarps : kNormThreads / s.lanes) : 0, st, a);   // (32 KB at most)
 }
 template <class T, int V, bool RAGGED, bool BWD> int launch_norm_lanes(const NormArgs& a, const NormShape& s, cudaStream_t st) {
-    if (s.each == 16) return s.lanes == 32 ? launch_norm<T, V, 16, 32, RAGGED, BWD>(a, s, st) : launch_norm<T, V, 16, 0, RAGGED, BWD>(a, s, st);
-    if constexpr (!RAGGED) {   // (more than 32 columns: 4 lanes and more)
+    constexpr bool kSixteen = sixteen_elements(sizeof(T), V > 1, RAGGED, BWD);   // (else 16 elements are more than 2048 columns: 256 lanes)
+    if constexpr (kSixteen)
+        if (s.each == 16 && s.lanes == 32) return launch_norm<T, V, 16, 32, RAGGED, BWD>(a, s, st);
+    if (s.each == 16) return launch_norm<T, V, 16, 0, RAGGED, BWD>(a, s, st);
+    if constexpr (!RAGGED) {   // (more than 32 columns: 8 lanes and more)
         if (s.lanes == 1) return launch_norm<T, V, 8, 1, RAGGED, BWD>(a, s, st);
         if (s.lanes == 2) return launch_norm<T, V, 8, 2, RAGGED, BWD>(a, s, st);
         if (s.lanes == 4) return launch_norm<T, V, 8, 4, RAGGED, BWD>(a, s, st);
     }
     if (s.lanes == 8) return launch_norm<T, V, 8, 8, RAGGED, BWD>(a, s, st);
     if (s.lanes == 16) return launch_norm<T, V, 8, 16, RAGGED, BWD>(a, s, st);
-    if (s.lanes == 32) return launch_norm<T, V, 8, 32, RAGGED, BWD>(a, s, st);
-    return launch_norm<T, V, 8, 0, RAGGED, BWD>(a, s, st);
+    if constexpr (kSixteen) return launch_norm<T, V, 8, 32, RAGGED, BWD>(a, s, st);   // (8 elements are up to 256 columns)
+    else return s.lanes == 32 ? launch_norm<T, V, 8, 32, RAGGED, BWD>(a, s, st) : launch_norm<T, V, 8, 0, RAGGED, BWD>(a, s, st);
 }
 template <class T, bool BWD> int norm(NormArgs a, const NormShape& s, cudaStream_t st) {
     a.lanes = s.lanes;
