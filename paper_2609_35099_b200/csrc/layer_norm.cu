@@ -399,6 +399,7 @@ int e3j_layer_norm_fwd(int dtype, int64_t rows, int n, const void* x, const void
     if (!x || !y) return E3J_ERR_INVALID_ARG;
     const uintptr_t odd = dtype == E3J_F32 ? 3u : 1u;
     if (((uintptr_t)x | (uintptr_t)weight | (uintptr_t)bias | (uintptr_t)y) & odd) return E3J_ERR_INVALID_ARG;
+    if ((uintptr_t)n_real & 3u) return E3J_ERR_INVALID_ARG;
     NormArgs a{};
     a.rows = rows; a.n = n; a.eps = (float)eps; a.inverse_n = 1.f / (float)n; a.act = act;
     a.x = x; a.weight = weight; a.bias = bias; a.n_real = n_real; a.out = y;
@@ -424,7 +425,7 @@ int e3j_layer_norm_bwd(int dtype, int64_t rows, int n, const void* x, const void
     const size_t size = dtype == E3J_F32 ? 4 : 2;
     const uintptr_t arrays = (uintptr_t)x | (uintptr_t)weight | (uintptr_t)bias | (uintptr_t)grad_y | (uintptr_t)grad_x |
                              (uintptr_t)grad_weight | (uintptr_t)grad_bias;
-    if (arrays & (size - 1)) return E3J_ERR_INVALID_ARG;
+    if ((arrays & (size - 1)) || ((uintptr_t)n_real & 3u)) return E3J_ERR_INVALID_ARG;
     if (rows == 0) {   // sums over no rows
         if (grad_weight) E3J_CUDA_TRY(cudaMemsetAsync(grad_weight, 0, size * n, st));
         if (grad_bias) E3J_CUDA_TRY(cudaMemsetAsync(grad_bias, 0, size * n, st));

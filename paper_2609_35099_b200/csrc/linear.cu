@@ -82,6 +82,7 @@ int e3j_linear_fwd(int dtype, int64_t rows, int n_in, int n_out, const void* x, 
     if (!x || !W || !y) return E3J_ERR_INVALID_ARG;
     const uintptr_t odd = dtype == E3J_F32 ? 3u : 1u;
     if (((uintptr_t)x | (uintptr_t)W | (uintptr_t)b | (uintptr_t)residual | (uintptr_t)y) & odd) return E3J_ERR_INVALID_ARG;
+    if ((uintptr_t)n_real & 3u) return E3J_ERR_INVALID_ARG;
     LinArgs a{};
     a.rows = rows; a.n_in = n_in; a.n_out = n_out; a.n_real = n_real;
     if (int rc = status_word(&a.status)) return rc;
@@ -102,7 +103,7 @@ int e3j_linear_bwd(int dtype, int64_t rows, int n_in, int n_out, const void* x, 
     const size_t size = dtype == E3J_F32 ? 4 : 2;
     const uintptr_t arrays = (uintptr_t)x | (uintptr_t)W | (uintptr_t)b | (uintptr_t)grad_y | (uintptr_t)grad_x |
                              (uintptr_t)grad_W | (uintptr_t)grad_b;
-    if (arrays & (size - 1)) return E3J_ERR_INVALID_ARG;
+    if ((arrays & (size - 1)) || ((uintptr_t)n_real & 3u)) return E3J_ERR_INVALID_ARG;
     if (rows == 0) {   // sums over no rows
         if (grad_W) E3J_CUDA_TRY(cudaMemsetAsync(grad_W, 0, size * n_in * n_out, st));
         if (grad_b) E3J_CUDA_TRY(cudaMemsetAsync(grad_b, 0, size * n_out, st));

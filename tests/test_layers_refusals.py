@@ -102,3 +102,11 @@ def test_a_double_arrives_wherever_it_stands():
         with pytest.raises(TypeError):
             e3j._native.call_real(*bad)
     assert e3j._native.same_device(torch.zeros(3), None) == -1 and e3j._native.same_device(1) == -1
+
+
+def test_a_count_of_real_rows_off_its_alignment():
+    for n_real in (P + 1, P + 2):
+        assert linear_fwd(n_real=n_real) == BAD
+        assert LIB.e3j_linear_bwd(0, 5, 4, 3, P, P, P, P, 1, n_real, P, P, P, None, 0, None) == BAD
+        assert LIB.e3j_layer_norm_fwd(0, 5, 4, P, P, P, 1e-5, 1, n_real, P, None) == BAD
+        assert LIB.e3j_layer_norm_bwd(0, 5, 4, P, P, P, P, 1e-5, 1, n_real, P, P, P, None, 0, None) == BAD
