@@ -134,6 +134,7 @@ PyObject* call_real(PyObject*, PyObject* const* args, Py_ssize_t n) {
 // same_device(x, tensors...) -> x's device index where x and all that are not None (or truth values) are tensors on it, and it is the
 // current one; else -1: the binding looks into it.
 PyObject* same_device(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS   // (the current device is a call of the runtime, which throws where it fails)
     int device = -1;
     for (Py_ssize_t i = 0; i < n; ++i) {
         if (i > 0 && (args[i] == Py_None || PyBool_Check(args[i]))) continue;
@@ -143,6 +144,7 @@ PyObject* same_device(PyObject*, PyObject* const* args, Py_ssize_t n) {
         device = (int)t.get_device();
     }
     return PyLong_FromLong(device >= 0 && c10::impl::VirtualGuardImpl(at::kCUDA).getDevice().index() == device ? device : -1);
+    END_HANDLE_TH_ERRORS
 }
 
 // set_slow(dev_ptr, empty): what the two functions above fall back on
