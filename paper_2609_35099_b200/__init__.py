@@ -776,6 +776,12 @@ def _wanted(flag, shape, dtype, like):
     return _empty(shape, dtype, like) if flag is True else None if flag is False else flag
 
 
+def _columns(W):
+    if not isinstance(W, _torch_module.Tensor) or W.dim() != 2:
+        raise TypeError("W must be a CUDA tensor [n_in, n_out]")
+    return W.shape[1]
+
+
 def e3j_linear_fwd(x, W, b=None, residual=None, act: int = E3J_ACT_NONE, n_real=None, out=None, stream=None):
     """act(x W + b) + residual: x [rows, n_in], W [n_in, n_out], b [n_out], residual [rows, n_out], all float32 or all
     bfloat16.  n_real: int32 CUDA tensor of one element, the number of real rows of a padded list (rowptr[-1:]); the
@@ -784,7 +790,7 @@ def e3j_linear_fwd(x, W, b=None, residual=None, act: int = E3J_ACT_NONE, n_real=
     if elsewhere is not None:
         with elsewhere:
             return e3j_linear_fwd(x, W, b, residual, act, n_real, out, stream)
-    dtype, (rows, n_in), n_out = x.dtype, x.shape, W.shape[-1]
+    dtype, (rows, n_in), n_out = x.dtype, x.shape, _columns(W)
     if out is None:
         out = _empty((rows, n_out), dtype, x)
     _run("e3j_linear_fwd", code, rows, n_in, n_out, _dev_ptr(x, dtype, None, "x"), _dev_ptr(W, dtype, (n_in, n_out), "W"),
@@ -805,7 +811,7 @@ def e3j_linear_bwd(x, W, b, grad_y, act: int = E3J_ACT_NONE, n_real=None, grad_x
     if elsewhere is not None:
         with elsewhere:
             return e3j_linear_bwd(x, W, b, grad_y, act, n_real, grad_x, grad_W, grad_b, workspace, stream)
-    dtype, (rows, n_in), n_out = x.dtype, x.shape, W.shape[-1]
+    dtype, (rows, n_in), n_out = x.dtype, x.shape, _columns(W)
     grad_x, grad_W = _wanted(grad_x, (rows, n_in), dtype, x), _wanted(grad_W, (n_in, n_out), dtype, x)
     grad_b = _wanted(grad_b, (n_out,), dtype, x)
     alone = grad_W is None and grad_b is None and (act == E3J_ACT_NONE or n_in <= 64 and n_out <= 64)   # needs no workspace

@@ -104,3 +104,11 @@ def test_with_an_activation_beyond_64_columns_room_for_gz_is_still_asked_for():
     gx = torch.empty_like(x)
     assert bwd_without_room(x, W, g, SILU, gx, 0) == e3j.E3J_ERR_WORKSPACE
     assert torch.equal(e3j.e3j_linear_bwd(x, W, None, g, SILU, grad_W=False, grad_b=False)[0], e3j.e3j_linear_bwd(x, W, None, g, SILU)[0])
+
+
+def test_a_missing_or_flat_W_is_named():
+    x, g = torch.randn(5, 4, device="cuda"), torch.randn(5, 3, device="cuda")
+    for W in (None, [1.0], torch.randn(12, device="cuda"), torch.tensor(1.0, device="cuda")):
+        for call in (lambda: e3j.e3j_linear_fwd(x, W), lambda: e3j.e3j_linear_bwd(x, W, None, g)):
+            with pytest.raises(TypeError, match="W must be a CUDA tensor"):
+                call()
