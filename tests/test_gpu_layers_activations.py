@@ -90,3 +90,21 @@ def test_gelu_is_as_exact_as_the_elementary_form():
         want = x64 * 0.5 * torch.erfc(-x64 / 2 ** 0.5)
         y = e3j.e3j_linear_fwd(x, torch.eye(64, device="cuda"), act=GELU)
         assert (y.double() - want).norm() <= U * want.norm(), scale
+
+
+@pytest.mark.parametrize("n_in,n_out", [(64, 64), (33, 130), (512, 200)])
+def test_an_infinity_in_x(n_in, n_out):
+    """bfloat16: infinities with the signs of W's row; float32, whose values are cut into terms: NaN.  The other rows as without it."""
+    for dtype in (torch.float32, torch.bfloat16):
+        x, W = torch.randn(300, n_in, device="cuda").to(dtype), (torch.rand(n_in, n_out, device="cuda") - 0.5).to(dtype)
+        W[5] = torch.where(W[5] == 0, torch.ones_like(W[5]), W[5])
+        want = e3j.e3j_linear_fwd(x, W)
+        x[7, 5], x[200, 5] = INF, -INF
+        y = e3j.e3j_linear_fwd(x, W)
+        rest = torch.ones(300, dtype=torch.bool, device="cuda")
+        rest[[7, 200]] = False
+        assert torch.equal(y[rest], want[rest])
+        if dtype == torch.bfloat16:
+            assert torch.equal(y[7].float(), torch.sign(W[5].float()) * INF) and torch.equal(y[200], -y[7])
+        else:
+            assert torch.isnan(y[[7, 200]]).all()

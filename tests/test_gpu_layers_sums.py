@@ -5,6 +5,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
+import layer_util as ref
 import paper_2609_35099_b200 as e3j
 
 pytestmark = pytest.mark.gpu
@@ -103,3 +104,23 @@ def test_layer_norm_s_sums_keep_float32_accuracy(rows, n):
     xh = d / torch.sqrt((d * d).mean(1, keepdim=True) + 1e-5)
     for got, want in ((gw, (g.double() * xh).sum(0)), (gc, g.double().sum(0))):
         assert (got.double() - want).norm() <= 40 * U * want.norm()
+
+
+@pytest.mark.parametrize("rows,real", [(20003, None), (20003, 12345), (389, 200), (389, 1), (389, 0)])
+@pytest.mark.parametrize("n_in,n_out", [(300, 161), (512, 256), (400, 64), (257, 130), (64, 320), (97, 401)])
+def test_two_chains_over_many_tiles_and_padded(rows, real, n_in, n_out):
+    """More than one tile a block, and lists that end inside one, where the forward's or grad_x's contraction is two chains."""
+    rng = np.random.default_rng(n_in)
+    kept = rows if real is None else real
+    arrays = [rng.standard_normal(s) * k for s, k in (((rows, n_in), 1), ((n_in, n_out), n_in ** -0.5), ((n_out,), 0.5), ((rows, n_out), 1))]
+    x, W, b, g = (torch.from_numpy(a).float().cuda() for a in arrays)
+    x_, W_, b_, g_ = (t.double().cpu().numpy() for t in (x[:kept], W, b, g[:kept]))
+    x[kept:], g[kept:] = float("nan"), float("nan")
+    count = None if real is None else torch.tensor([real], dtype=torch.int32, device="cuda")
+    y = e3j.e3j_linear_fwd(x, W, b, g, ref.ACTS["silu"], n_real=count)
+    ref.assert_within(y[:kept], *ref.linear_fwd(x_, W_, b_, g_, "silu", U), "y")
+    got = e3j.e3j_linear_bwd(x, W, b, g, ref.ACTS["gelu"], n_real=count)
+    want, bounds = ref.linear_bwd(x_, W_, b_, g_, "gelu", U)
+    for t, v, e, what in zip((got[0][:kept], *got[1:]), want, bounds, ("grad_x", "grad_W", "grad_b")):
+        ref.assert_within(t, v, e, what)
+    assert (y[kept:] == 0).all() and (got[0][kept:] == 0).all() and e3j.e3j_linear_status() == 0
