@@ -330,7 +330,8 @@ int e3j_conv_radial_bwd(const e3j_plan* plan, int64_t n_nodes, int64_t n_edges, 
 
 /* Linear layer: y = act(x W + b) + residual with x [rows, n_in], W [n_in, n_out], b [n_out] or NULL, residual [rows, n_out] or
  * NULL, y [rows, n_out]; widths from 1 to 4096.  The products run on the tensor cores with float32 accuracy for float32 tensors (each
- * as the sum of three bfloat16 terms); a row with an infinity or a NaN in x comes out as NaN, and so does a column of such a W.
+ * as the sum of three bfloat16 terms); so a float32 row with an infinity or a NaN in x comes out as NaN, and so does a column of such a W
+ * (bfloat16: infinities multiply and add as usual).
  * Backward: gz = grad_y act'(x W + b), formed again from x, W and b (the forward keeps nothing); grad_x = gz W^T, grad_W = x^T gz,
  * grad_b = sum over rows of gz; the residual's gradient is grad_y itself.  Any of grad_x, grad_W, grad_b may be NULL (not wanted).
  * Workspace: 256-byte aligned, e3j_linear_bwd_workspace_bytes() (0: none is needed, NULL will do); calls that overlap on the GPU must

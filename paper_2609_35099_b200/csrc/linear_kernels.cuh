@@ -30,7 +30,7 @@
 // A block is one per SM and has three roles: eight warps fetch, split and store operands (one chunk in registers ahead; bfloat16 rows
 // that start on 16 bytes go to shared memory by cp.async, up to four chunks ahead, or in large calls as boxes of a tensor map, which one
 // thread asks for, as many ahead as there are stages), one issues the tensor-core instructions, eight
-// read accumulators and finish tiles.  Operand stages and two accumulator sets stand between them.  As one role of 256 threads
+// (bfloat16: sixteen) read accumulators and finish tiles.  Operand stages and accumulator sets stand between them.  As one role of 256 threads
 // that took turns, two blocks an SM, 160 900 x 64 -> 64 float32 took 25.7 us instead of 22.4.  Waits are bounded (fast::mbar_wait).
 #pragma once
 #include "layer_common.cuh"
